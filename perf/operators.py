@@ -1,0 +1,376 @@
+"""Operators of sampled decoding over long contexts, as cases whose time can be measured.
+
+  store   key and value rows into an 8-bit cache (e4m3 codes, a power-of-two scale for each token and kv head), and out again
+  attend  grouped-query attention of up to 8 query rows over such a cache
+  probs   the distributions that temperature, top-k, top-p and min-p make of rows of logits
+  sample  a draw from such a distribution with a given uniform number
+  verify  the accept / resample rule between such distributions, over the rows of a verification
+
+With `own` false a pass is the operator's plain form in elementary torch operations; with `own` true it is the call of the
+library's entry point.  Inputs are made on the GPU from the seed alone.
+
+Definitions.  A row of an 8-bit cache entry x [head_dim] is stored as codes c = e4m3(x / 2^e), rounded to nearest even, with e the smallest exponent
+(not below -126) for which max |x| <= 448 * 2^e.  A filter orders a row's ids by logit, largest first, equal ones by id; it
+keeps the first top_k of them; of those, the ones before which less than top_p of their weight lies; and of those the ones whose
+probability is at least min_p times the largest.  A value of 0 (top_p: 0 or 1) leaves that step out.  Draws go by inversion of the cumulative distribution
+in id order: the first id whose cumulative weight exceeds u times the total.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda:0"
+# (query heads, kv heads, head_dim) of the model shapes in use here, and the same with one kv head
+HEADS = [(4, 4, 64), (4, 2, 64), (32, 8, 128), (40, 40, 128), (64, 16, 128), (16, 1, 128)]
+
+
+# ---- the cases ---------------------------------------------------------------------------------------------
+
+def listed():
+    return [
+        # one token of plain decoding joins the cache
+        dict(name="store_one", op="store", Hq=32, Hkv=8, dh=128, ctx=4095, n=1),
+        # a full pass of a long prompt, at a position that is a multiple of nothing
+        dict(name="store_prompt", op="store", Hq=32, Hkv=8, dh=128, ctx=333, n=1024),
+        # the shortest call: a small model, a few pending rows, a context inside one block
+        dict(name="attend_tiny", op="attend", Hq=4, Hkv=2, dh=64, ctx=47, m=5),
+        # plain decoding in the middle of the range
+        dict(name="attend_4096", op="attend", Hq=32, Hkv=8, dh=128, ctx=4096, m=1),
+        # no grouping of heads, an odd context
+        dict(name="attend_mha_777", op="attend", Hq=40, Hkv=40, dh=128, ctx=777, m=2),
+        # a long context and all rows that may be pending
+        dict(name="attend_long", op="attend", Hq=32, Hkv=8, dh=128, ctx=131072, m=8),
+        # the distribution of one newly read row, a small vocabulary
+        dict(name="probs_small", op="probs", vocab=2048, rows=1, T=0.8, top_k=50, top_p=0.9, min_p=0.0),
+        # the distributions of all rows of a verification
+        dict(name="probs_rows", op="probs", vocab=128256, rows=8, T=0.7, top_k=0, top_p=0.95, min_p=0.0),
+        # the next token: the usual filters together
+        dict(name="sample_usual", op="sample", vocab=128256, T=0.8, top_k=50, top_p=0.9, min_p=0.02),
+        # the next token: the nucleus alone, hot, which keeps thousands of ids
+        dict(name="sample_nucleus", op="sample", vocab=32016, T=1.2, top_k=0, top_p=0.98, min_p=0.0),
+        # five drafts against the final layer
+        dict(name="verify_drafts", op="verify", vocab=128256, rows=6, T=0.8, top_k=0, top_p=0.9, min_p=0.0),
+        # two drafts, a smaller vocabulary, the usual filters together
+        dict(name="verify_short", op="verify", vocab=32016, rows=3, T=1.0, top_k=40, top_p=0.95, min_p=0.05),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["store", "attend", "attend", "probs", "sample", "verify"])
+    if op in ("store", "attend"):
+        Hq, Hkv, dh = rng.choice(HEADS)
+        width = Hkv * dh
+        if op == "store":
+            return dict(op=op, Hq=Hq, Hkv=Hkv, dh=dh, ctx=_log_int(rng, 1, 8192) - 1, n=_log_int(rng, 1, 1024 * 1024 // width))
+        # no more products, and no more of a cache, than the largest listed call has
+        m = rng.randint(1, 8)
+        most = min(131072 * 1024 // width, 8 * 131072 * 4096 // (m * Hq * dh), 262144)
+        return dict(op=op, Hq=Hq, Hkv=Hkv, dh=dh, ctx=_log_int(rng, 8, most), m=m)
+    case = dict(op=op, vocab=_log_int(rng, 300, 128256), T=round(rng.uniform(0.4, 1.5), 3), top_k=0, top_p=0.0, min_p=0.0)
+    if op != "sample":
+        case["rows"] = rng.randint(1, 8) if op == "probs" else rng.randint(1, 6)
+    which = rng.randint(1, 7)
+    if which & 1:
+        case["top_k"] = _log_int(rng, 1, 2 * case["vocab"])
+    if which & 2:
+        case["top_p"] = round(rng.uniform(0.3, 0.999), 4)
+    if which & 4:
+        case["min_p"] = round(math.exp(rng.uniform(math.log(1e-4), math.log(0.5))), 6)
+    return case
+
+
+def work(case):
+    if case["op"] == "store":
+        values = 2 * case["n"] * case["Hkv"] * case["dh"]
+        scales = 2 * case["n"] * case["Hkv"]
+        # rows in, codes and scales out; codes and scales in, values out
+        return dict(bytes=4 * values + 2 * (values + scales) + 4 * values, flops=4 * values)
+    if case["op"] == "attend":
+        rows = case["m"] * case["Hq"]
+        return dict(bytes=case["ctx"] * case["Hkv"] * (2 * case["dh"] + 2) + 8 * rows * case["dh"], flops=4 * rows * case["dh"] * case["ctx"])
+    V = case["vocab"]
+    if case["op"] == "probs":
+        return dict(bytes=8 * V * case["rows"], flops=8 * V * case["rows"])
+    rows = 1 if case["op"] == "sample" else 2 * case["rows"] - 1
+    return dict(bytes=4 * V * rows, flops=8 * V * rows)
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------
+
+def _gen(seed, salt):
+    g = torch.Generator(device=DEV)
+    g.manual_seed((int(seed) * 1000003 + salt) % (1 << 62))
+    return g
+
+
+def _kv_rows(case, seed, n, salt):
+    """Rotated keys and values of n positions, float32 [n, Hkv, dh]: keys with a few strong dimensions, values whose size differs by token."""
+    g = _gen(seed, salt)
+    Hkv, dh = case["Hkv"], case["dh"]
+    k = torch.randn((n, Hkv, dh), generator=g, device=DEV)
+    k[:, :, :: dh // 4] *= 4.0
+    v = torch.randn((n, Hkv, dh), generator=g, device=DEV)
+    v *= torch.exp(0.7 * torch.randn((n, Hkv, 1), generator=g, device=DEV))
+    return k, v
+
+
+def _logits(case, seed, rows):
+    """Rows of logits with the heavy tail of a language model's."""
+    g = _gen(seed, 11)
+    V = case["vocab"]
+    rank = torch.argsort(torch.rand((rows, V), generator=g, device=DEV), dim=-1)
+    return 14.0 - 1.3 * torch.log1p(rank.float()) + 0.4 * torch.randn((rows, V), generator=g, device=DEV)
+
+
+def _uniforms(seed, n):
+    # (in float32 and below 1, as callers supply them)
+    return np.random.default_rng([int(seed) % (1 << 31), 17]).random(n).astype(np.float32) * np.float32(1 - 2.0 ** -20)
+
+
+def _f32(x):
+    return float(np.float32(x))
+
+
+def _filter(case):
+    """(temperature, top_k, top_p, min_p), numbers as float32 holds them."""
+    return _f32(case["T"]), int(case["top_k"]), _f32(case["top_p"]), _f32(case["min_p"])
+
+
+def _small_model(Hq, Hkv, dh, vocab, max_pos, kv8):
+    """A handle of the library with the head counts, or the vocabulary, of the case; its weights do not matter here."""
+    from paper_2506_03700_amd import binding, synth
+    s = synth.ModelShape("operators", 1, 64, Hq, Hkv, dh, 64, vocab, 10000.0, (), synth.BF16, True)
+    sizes = dict(attn_norm=(64,), wq=(Hq * dh, 64), wk=(Hkv * dh, 64), wv=(Hkv * dh, 64), wo=(64, Hq * dh), ffn_norm=(64,),
+                 w_gate=(64, 64), w_up=(64, 64), w_down=(64, 64))
+    w = {"layers.0." + n: np.zeros(v, dtype=np.uint16) for n, v in sizes.items()}
+    w["embed"] = np.zeros((vocab, 64), dtype=np.uint16)
+    w["final_norm"] = np.zeros((64,), dtype=np.uint16)
+    w["lm_head"] = w["embed"]
+    return binding.Model(s, w, max_pos, kv8=kv8)
+
+
+def prepare(case, seed):
+    op = case["op"]
+    st = dict(case=case, op=op)
+    if op in ("store", "attend"):
+        ctx, n = case["ctx"], case.get("n", 0)
+        if own:
+            st["model"] = _small_model(case["Hq"], case["Hkv"], case["dh"], 256, ctx + max(n, 1), True)
+        if op == "store":
+            st["k"], st["v"] = _kv_rows(case, seed, n, 3)
+            if own:
+                st["model"].kv_set_len(1, ctx)
+            return st
+        st["q"] = 1.5 * torch.randn((case["m"], case["Hq"], case["dh"]), generator=_gen(seed, 5), device=DEV)
+        # the newest rows' queries: row r sees the positions up to its own
+        st["pos"] = [max(0, ctx - case["m"] + r) for r in range(case["m"])]
+        k, v = _kv_rows(case, seed, ctx, 3)
+        if own:
+            st["model"].ad_kv8_append(1, k, v, 0)
+        else:
+            st["see"] = torch.tensor(st["pos"], device=DEV)
+            st["cache"] = [_quantise(x) for x in (k, v)]
+        return st
+    m = case.get("rows", 1)
+    T, top_k, top_p, min_p = _filter(case)
+    z = _logits(case, seed, m)
+    st["u"] = u = _uniforms(seed, 3 * m)
+    if op == "verify" and m > 1:
+        # an earlier layer's logits for the same rows: near the final ones
+        st["draft_logits"] = zq = z[: m - 1] + 0.5 * torch.randn((m - 1, case["vocab"]), generator=_gen(seed, 13), device=DEV)
+        q = _plain_probs(zq, T, top_k, top_p, min_p)
+        st["draft"] = _plain_draw(q, torch.from_numpy(u[2 * m : 3 * m - 1]).to(DEV)).cpu().numpy().astype(np.int32)
+    elif op == "verify":
+        st["draft_logits"], st["draft"] = z[:0], np.zeros(0, np.int32)
+    st["logits"] = z[0].contiguous() if op == "sample" else z
+    if own:
+        from paper_2506_03700_amd import binding
+        st["model"] = _small_model(1, 1, 64, case["vocab"], 8, False)
+        st["filter"] = binding.Filter(T, top_k, top_p, min_p)
+    else:
+        # (the plain form takes its draws and drafts as tensors)
+        st["u_dev"] = torch.from_numpy(u).to(DEV)
+        if op == "verify":
+            st["draft_dev"] = torch.from_numpy(st["draft"]).to(DEV).long()
+    return st
+
+
+# ---- one pass ----------------------------------------------------------------------------------------------
+
+def run(st):
+    op, case = st["op"], st["case"]
+    if own:
+        model = st["model"]
+        if op == "store":
+            # the rows take the place of what an earlier step left behind the context
+            model.kv_truncate(case["ctx"])
+            model.ad_kv8_append(1, st["k"], st["v"], case["ctx"])
+            return model.ad_kv8_read(1, case["ctx"], case["n"])
+        if op == "attend":
+            return model.ad_kv8_attend(1, st["q"], st["pos"])
+        if op == "probs":
+            return model.ad_filtered_probs(st["logits"], st["filter"])
+        if op == "sample":
+            return model.ad_sample_filtered(st["logits"], st["filter"], float(st["u"][0]))
+        m = case["rows"]
+        u = st["u"]
+        return model.ad_verify_filtered(st["logits"], st["draft_logits"], st["draft"], st["filter"], u[: m - 1], u[m : 2 * m - 1], float(u[m - 1]))
+    if op == "store":
+        return tuple(_values(*_quantise(x)) for x in (st["k"], st["v"]))
+    if op == "attend":
+        return _plain_attend(st)
+    T, top_k, top_p, min_p = _filter(case)
+    if op == "probs":
+        return _plain_probs(st["logits"], T, top_k, top_p, min_p).float()
+    if op == "sample":
+        p = _plain_probs(st["logits"][None], T, top_k, top_p, min_p)
+        token = _plain_draw(p, st["u_dev"][:1])[0]
+        return token, p[0, token].float()
+    return _plain_verify(st, T, top_k, top_p, min_p)
+
+
+# ---- plain forms -------------------------------------------------------------------------------------------
+
+def _quantise(x):
+    """Codes (e4m3) and scales (a power of two for each row of the last dimension)."""
+    mantissa, exponent = torch.frexp(x.abs().amax(dim=-1))           # mantissa in [0.5, 1)
+    e = (exponent - 9 + (mantissa > 0.875).int()).clamp(min=-126)
+    scale = torch.ldexp(torch.ones_like(mantissa), e)
+    return (x / scale[..., None]).to(torch.float8_e4m3fn), scale
+
+
+def _values(codes, scale):
+    return codes.float() * scale[..., None]
+
+
+def _plain_attend(st):
+    q, (k, v) = st["q"], (_values(*c) for c in st["cache"])
+    m, Hq, dh = q.shape
+    n, Hkv, _ = k.shape
+    rows = q.reshape(m, Hkv, Hq // Hkv, dh).transpose(0, 1).reshape(Hkv, -1, dh)                # [Hkv, m * G, dh]
+    s = torch.matmul(rows, k.permute(1, 2, 0).contiguous()) / math.sqrt(dh)
+    hidden = torch.arange(n, device=q.device)[None, :] > st["see"].repeat_interleave(Hq // Hkv)[:, None]
+    s = s.masked_fill(hidden, -math.inf)
+    p = torch.exp(s - s.amax(dim=-1, keepdim=True))
+    o = torch.matmul(p, v.permute(1, 0, 2).contiguous()) / p.sum(dim=-1, keepdim=True)
+    return o.reshape(Hkv, m, Hq // Hkv, dh).transpose(0, 1).reshape(m, Hq * dh)
+
+
+def _plain_probs(z, T, top_k, top_p, min_p):
+    """Filtered probabilities of each row, in 64 bits."""
+    x = z.double()
+    x = (x - x.amax(dim=-1, keepdim=True)) / T
+    s, ids = torch.sort(x, dim=-1, descending=True, stable=True)
+    w = torch.exp(s)
+    keep = w >= min_p
+    if top_k:
+        w[:, top_k:] = 0.0
+    if 0.0 < top_p < 1.0:
+        keep &= torch.cumsum(w, dim=-1) - w < top_p * w.sum(dim=-1, keepdim=True)
+    w = w * keep
+    return torch.zeros_like(w).scatter_(-1, ids, w / w.sum(dim=-1, keepdim=True))
+
+
+def _plain_draw(w, u):
+    """Of each row the first id whose cumulative weight exceeds u times the total."""
+    c = torch.cumsum(w, dim=-1)
+    return (c <= u.double()[:, None] * c[:, -1:]).sum(dim=-1).clamp(max=w.shape[-1] - 1)
+
+
+def _plain_verify(st, T, top_k, top_p, min_p):
+    m = st["case"]["rows"]
+    u = st["u_dev"].double()
+    p = _plain_probs(st["logits"], T, top_k, top_p, min_p)
+    q = torch.zeros_like(p)                                           # (behind the last row there is no draft)
+    ratio = torch.zeros(0, device=p.device)
+    n = torch.zeros((), dtype=torch.long, device=p.device)
+    if m > 1:
+        q[: m - 1] = _plain_probs(st["draft_logits"], T, top_k, top_p, min_p)
+        t = st["draft_dev"][:, None]
+        r = (p[: m - 1].gather(1, t) / q[: m - 1].gather(1, t))[:, 0]
+        taken = torch.cumprod((u[: m - 1] < r.clamp(max=1.0)).long(), 0)
+        n = taken.sum()
+        ratio = torch.where(torch.arange(m - 1, device=p.device) <= n, r, torch.zeros_like(r)).float()
+    rest = (p[n] - q[n]).clamp(min=0.0)
+    w = torch.where(rest.sum() > 0, rest, p[n])
+    at = torch.where(n < m - 1, m + n, m - 1)                         # the draw for a replacement, or for the token behind the last row
+    return n, _plain_draw(w[None], u[at][None])[0], ratio
+
+
+# ---- the same from the definitions, in 64 bits -------------------------------------------------------------
+
+def exact(case, seed):
+    op = case["op"]
+    if op == "store":
+        return tuple(_exact_values(x) for x in _kv_rows(case, seed, case["n"], 3))
+    if op == "attend":
+        k, v = (_exact_values(x) for x in _kv_rows(case, seed, case["ctx"], 3))
+        m, Hq, dh = case["m"], case["Hq"], case["dh"]
+        q = 1.5 * torch.randn((m, Hq, dh), generator=_gen(seed, 5), device=DEV)
+        G = Hq // case["Hkv"]
+        out = torch.empty((m, Hq, dh), dtype=torch.float64, device=DEV)
+        for r in range(m):
+            see = max(0, case["ctx"] - m + r) + 1
+            for h in range(Hq):
+                s = torch.mv(k[:see, h // G], q[r, h].double()) * dh ** -0.5
+                p = torch.softmax(s, 0)
+                out[r, h] = torch.mv(v[:see, h // G].t(), p)
+        return out.reshape(m, Hq * dh)
+    T, top_k, top_p, min_p = _filter(case)
+    m = case.get("rows", 1)
+    z = _logits(case, seed, m)
+    P = np.stack([_exact_row(r, T, top_k, top_p, min_p) for r in z.double().cpu().numpy()])
+    if op == "probs":
+        return P
+    u = _uniforms(seed, 3 * m).astype(np.float64)
+    if op == "sample":
+        token = _exact_draw(P[0], u[0])
+        return token, np.float64(P[0, token])
+    ratio = np.zeros(m - 1)
+    if m > 1:
+        zq = z[: m - 1] + 0.5 * torch.randn((m - 1, case["vocab"]), generator=_gen(seed, 13), device=DEV)
+        Q = [_exact_row(r, T, top_k, top_p, min_p) for r in zq.double().cpu().numpy()]
+        for k in range(m - 1):
+            t = _exact_draw(Q[k], u[2 * m + k])
+            ratio[k] = P[k, t] / Q[k][t]
+            if not u[k] < ratio[k]:
+                rest = np.maximum(P[k] - Q[k], 0.0)
+                return k, _exact_draw(rest if rest.sum() > 0 else P[k], u[m + k]), ratio
+    return m - 1, _exact_draw(P[m - 1], u[m - 1]), ratio
+
+
+def _exact_values(x):
+    x = x.double()
+    top = x.abs().amax(dim=-1, keepdim=True)
+    e = torch.floor(torch.log2(top)) - 8
+    e = torch.where(top > 448.0 * torch.exp2(e), e + 1, e).clamp(min=-126)
+    y = x / torch.exp2(e)
+    # three bits behind the leading one, down to 2^-9
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(y / step) * step * torch.exp2(e)
+
+
+def _exact_row(z, T, top_k, top_p, min_p):
+    order = np.lexsort((np.arange(z.size), -z))
+    w = np.exp((z[order] - z.max()) / T)
+    n = min(top_k, z.size) if top_k else z.size
+    if 0.0 < top_p < 1.0:
+        before = np.concatenate([[0.0], np.cumsum(w[:n])])
+        n = int(np.searchsorted(before[:-1], top_p * before[-1], side="left"))
+    if min_p:
+        n = min(n, int(np.count_nonzero(w >= min_p)))
+    p = np.zeros(z.size)
+    p[order[:n]] = w[:n] / w[:n].sum()
+    return p
+
+
+def _exact_draw(w, u):
+    c = np.cumsum(w)
+    return min(int(np.searchsorted(c, u * c[-1], side="right")), w.size - 1)
