@@ -143,7 +143,7 @@ def _filter(case):
     return _f32(case["T"]), int(case["top_k"]), _f32(case["top_p"]), _f32(case["min_p"])
 
 
-def _small_model(Hq, Hkv, dh, vocab, max_pos, kv8):
+def _small_model(Hq, Hkv, dh, vocab, max_pos, kvq):
     """A handle of the library with the head counts, or the vocabulary, of the case; its weights do not matter here."""
     from paper_2506_03700_amd import binding, synth
     s = synth.ModelShape("operators", 1, 64, Hq, Hkv, dh, 64, vocab, 10000.0, (), synth.BF16, True)
@@ -153,7 +153,7 @@ def _small_model(Hq, Hkv, dh, vocab, max_pos, kv8):
     w["embed"] = np.zeros((vocab, 64), dtype=np.uint16)
     w["final_norm"] = np.zeros((64,), dtype=np.uint16)
     w["lm_head"] = w["embed"]
-    return binding.Model(s, w, max_pos, kv8=kv8)
+    return binding.Model(s, w, max_pos, kvq=kvq)
 
 
 def prepare(case, seed):
@@ -173,7 +173,7 @@ def prepare(case, seed):
         st["pos"] = [max(0, ctx - case["m"] + r) for r in range(case["m"])]
         k, v = _kv_rows(case, seed, ctx, 3)
         if own:
-            st["model"].ad_kv8_append(1, k, v, 0)
+            st["model"].ad_kvq_append(1, k, v, 0)
         else:
             st["see"] = torch.tensor(st["pos"], device=DEV)
             st["cache"] = [_quantise(x) for x in (k, v)]
@@ -211,10 +211,10 @@ def run(st):
         if op == "store":
             # the rows take the place of what an earlier step left behind the context
             model.kv_truncate(case["ctx"])
-            model.ad_kv8_append(1, st["k"], st["v"], case["ctx"])
-            return model.ad_kv8_read(1, case["ctx"], case["n"])
+            model.ad_kvq_append(1, st["k"], st["v"], case["ctx"])
+            return model.ad_kvq_read(1, case["ctx"], case["n"])
         if op == "attend":
-            return model.ad_kv8_attend(1, st["q"], st["pos"])
+            return model.ad_kvq_attend(1, st["q"], st["pos"])
         if op == "probs":
             return model.ad_filtered_probs(st["logits"], st["filter"])
         if op == "sample":
