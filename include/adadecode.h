@@ -106,6 +106,39 @@ ad_status ad_kv_set_len(ad_kv *, int32_t layer, int32_t len);   /* declare a pre
 /* Rollback after a rejected early prediction (Sec. 2.2): every layer's length becomes min(len, new_len). */
 ad_status ad_kv_truncate(ad_kv *, int32_t new_len);
 
+/* ---- 8-bit cache: about half the bytes of a 16-bit one, for models of every dtype.  A key or value vector x [head_dim] of one token and kv head
+ * is stored as e4m3 codes (four significant bits, largest value 448, no infinity) c = x / 2^e rounded to nearest even, with e the smallest exponent, not
+ * below -126, for which max |x| <= 448 * 2^e: an entry is off by at most 2^-4 of itself or, below 2^-13 of the vector's
+ * largest, by 2^-17 of that (vectors whose largest magnitude is below 2^-118: by 2^-136).  Entries that are infinite or no
+ * numbers are stored as no numbers and have no part in the scale; a query that sees such an entry gets an output that is no number, one that
+ * does not see it is not affected.  What is stored for a position depends on that position's vector alone: the same tokens leave the same cache
+ * however they are divided over calls, so that verified early predictions leave what plain decoding leaves.
+ *
+ * The handle is an ad_kv like any other: ad_layer_step(s) in AD_LAYER_KERNELS mode (AD_LAYER_FUSED: AD_ESTATE), ad_generate (prompts in passes of up to
+ * 1024 tokens for 16-bit models, if the storage has ad_kvq_bytes() bytes), ad_kv_len, ad_kv_set_len, ad_kv_truncate, ad_kv_destroy.
+ * Storage layout, stride = max_pos rounded up to a multiple of 64, one byte each, per layer (rounded up to 256 bytes):
+ *   K codes [kv head][position 0..stride)[head_dim], V codes [kv head][position / 64][head_dim][64 positions],
+ *   K scales [kv head][position 0..stride), V scales likewise: the exponent e plus 127.
+ * max_pos as for ad_kv_create; alignment of the storage too. */
+size_t    ad_kvq_bytes(const ad_config *, int32_t max_pos);
+ad_status ad_kvq_create(const ad_model *, void *kv_storage /*dev*/, size_t kv_storage_bytes, int32_t max_pos, void *stream,
+                        ad_kv **out);
+
+/* Appends n rows of keys (already rotated) and values to a layer of an 8-bit cache: k, v: dev fp32, row i at k + i * ld, [n_kv_heads][head_dim]
+ * each, 16-byte aligned, ld a multiple of 4 and >= n_kv_heads * head_dim.  pos0 must equal the layer's length, which grows by n; n is
+ * bounded by max_pos alone. */
+ad_status ad_kvq_append(const ad_model *, ad_kv *, int32_t layer, const void *k, const void *v, int64_t ld, int32_t pos0, int32_t n,
+                        void *stream);
+/* The values that positions pos0 .. pos0 + n - 1 of a layer stand for (all below the layer's length): k, v: dev fp32, as
+ * ad_kvq_append takes them (an entry that rounded up to 2^128 reads as infinity). */
+ad_status ad_kvq_read(const ad_model *, const ad_kv *, int32_t layer, int32_t pos0, int32_t n, void *k, void *v, int64_t ld, void *stream);
+/* The attention of a layer step by itself: out[r] = softmax(q[r] K^T / sqrt(head_dim)) V over positions 0..pos[r] of the layer, query head h
+ * against kv head h / (n_q_heads / n_kv_heads).  q: dev fp32 [m, n_q_heads, head_dim], already rotated; out: dev fp32 [m, n_q_heads * head_dim];
+ * both 16-byte aligned and apart from each other.  pos: host [m], in any order, each below the layer's length; m in 1..m_max.  Uses scratch in the
+ * cache's storage: calls on one cache must be stream-ordered. */
+ad_status ad_kvq_attend(const ad_model *, const ad_kv *, int32_t layer, const void *q, const int32_t *pos, int32_t m, void *out,
+                        void *stream);
+
 /* hidden[r] = embedding row of tokens[r].  tokens: host [m]; hidden: dev [m, d] fp32. */
 ad_status ad_embed(const ad_model *, const int32_t *tokens, int32_t m, void *hidden, void *stream);
 

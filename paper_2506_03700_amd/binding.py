@@ -28,7 +28,8 @@ EXPORTS = ["ad_workspace_bytes", "ad_model_create", "ad_model_destroy", "ad_kv_b
            "ad_kv_len", "ad_kv_set_len", "ad_kv_truncate", "ad_embed", "ad_layer_step", "ad_layer_steps", "ad_set_layer_mode", "ad_exit_head", "ad_verify",
            "ad_verify_static", "ad_exit_head_wait", "ad_verify_wait", "ad_sample_logits_wait", "ad_verify_sampled_wait",
            "ad_head_logits", "ad_sample_logits", "ad_verify_sampled", "ad_generate", "ad_layer_trace", "ad_profile_start", "ad_profile_stop", "ad_probe_stream",
-           "ad_last_error", "ad_version"]
+           "ad_last_error", "ad_version",
+           "ad_kvq_bytes", "ad_kvq_create", "ad_kvq_append", "ad_kvq_read", "ad_kvq_attend"]
 
 
 class Config(C.Structure):
@@ -96,6 +97,12 @@ def lib() -> C.CDLL:
         L.ad_kv_len.argtypes = [P, i32, C.POINTER(i32)]
         L.ad_kv_set_len.argtypes = [P, i32, i32]
         L.ad_kv_truncate.argtypes = [P, i32]
+        L.ad_kvq_bytes.restype = sz
+        L.ad_kvq_bytes.argtypes = [C.POINTER(Config), i32]
+        L.ad_kvq_create.argtypes = [P, P, sz, i32, P, C.POINTER(P)]
+        L.ad_kvq_append.argtypes = [P, P, i32, P, P, C.c_int64, i32, i32, P]
+        L.ad_kvq_read.argtypes = [P, P, i32, i32, i32, P, P, C.c_int64, P]
+        L.ad_kvq_attend.argtypes = [P, P, i32, P, P, i32, P, P]
         L.ad_embed.argtypes = [P, P, i32, P, P]
         L.ad_layer_step.argtypes = [P, P, i32, P, P, i32, P]
         L.ad_layer_steps.argtypes = [P, P, i32, i32, P, P, i32, P]
@@ -116,7 +123,7 @@ def lib() -> C.CDLL:
         L.ad_last_error.restype = C.c_char_p
         L.ad_version.restype = C.c_char_p
         for n in EXPORTS:
-            if n not in ("ad_workspace_bytes", "ad_kv_bytes", "ad_last_error", "ad_version"):
+            if n not in ("ad_workspace_bytes", "ad_kv_bytes", "ad_kvq_bytes", "ad_last_error", "ad_version"):
                 getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -154,8 +161,10 @@ def _stream_ptr(torch):
 class Model:
     """ad_model + ad_kv over torch device buffers.  Method names follow the C entry points."""
 
+    kvq = False      # whether the cache holds 8-bit entries
+
     def __init__(self, shape, weights: Dict[str, np.ndarray], max_pos: int, m_max: int = AD_M_MAX, device: str = "cuda:0",
-                 layer_mode: Optional[int] = None):
+                 layer_mode: Optional[int] = None, kvq: bool = False):
         import torch
         self.torch = torch
         self.shape = shape
@@ -198,9 +207,11 @@ class Model:
         torch.cuda.synchronize()
         del keep          # the originals may be freed once creation has been synchronised
         self.max_pos = max_pos
-        kv_bytes = self.L.ad_kv_bytes(C.byref(self.cfg), max_pos)
+        self.kvq = kvq
+        kv_bytes = (self.L.ad_kvq_bytes if kvq else self.L.ad_kv_bytes)(C.byref(self.cfg), max_pos)
         self.kv_storage = torch.zeros(kv_bytes, dtype=torch.uint8, device=self.device)
-        _check(self.L.ad_kv_create(self.model, C.c_void_p(self.kv_storage.data_ptr()), kv_bytes, max_pos, _stream_ptr(torch), C.byref(self.kv)))
+        _check((self.L.ad_kvq_create if kvq else self.L.ad_kv_create)(self.model, C.c_void_p(self.kv_storage.data_ptr()), kv_bytes, max_pos,
+                                                                      _stream_ptr(torch), C.byref(self.kv)))
         self._pinned = torch.zeros(64, dtype=torch.int32).pin_memory()
         if layer_mode is not None:
             self.ad_set_layer_mode(layer_mode)
@@ -254,6 +265,7 @@ class Model:
         """(K, V): K as [layer][kv head][position][head_dim], V as [layer][kv head][head_dim][position]
         (the library stores V transposed), positions 0..stride, of the storage dtype."""
         s, torch = self.shape, self.torch
+        assert not self.kvq, "an 8-bit cache has kvq_views"
         dt = {AD_F32: torch.float32, AD_BF16: torch.bfloat16, AD_F16: torch.float16}[s.dtype]
         half = s.n_kv_heads * self.kv_stride * s.head_dim
         flat = self.kv_storage[: s.n_layers * 2 * half * s.elem_bytes()].view(dt).view(s.n_layers, 2, half)
@@ -261,9 +273,27 @@ class Model:
         v = flat[:, 1].view(s.n_layers, s.n_kv_heads, s.head_dim, self.kv_stride)
         return k, v
 
+    def kvq_views(self):
+        """An 8-bit cache's storage, uint8: (K codes [layer][kv head][position][head_dim], V codes [layer][kv head][position / 64][head_dim][64],
+        K scales [layer][kv head][position], V scales likewise), positions 0..stride."""
+        s, n = self.shape, self.kv_stride
+        assert self.kvq
+        codes, scales = s.n_kv_heads * n * s.head_dim, s.n_kv_heads * n
+        size = (2 * (codes + scales) + 255) // 256 * 256
+        flat = self.kv_storage[: s.n_layers * size].view(s.n_layers, size)
+        part = lambda at, count, *shape: flat[:, at : at + count].unflatten(1, shape)
+        return (part(0, codes, s.n_kv_heads, n, s.head_dim), part(codes, codes, s.n_kv_heads, n // 64, s.head_dim, 64),
+                part(2 * codes, scales, s.n_kv_heads, n), part(2 * codes + scales, scales, s.n_kv_heads, n))
+
     def kv_fill(self, layer: int, k, v) -> None:
         """Write positions [0, n) of one layer from arrays [n, kv heads, head_dim] (benchmarks, tests)."""
         torch = self.torch
+        if self.kvq:
+            had = self.kv_len(layer)
+            self.kv_set_len(layer, 0)
+            self.ad_kvq_append(layer, *(torch.as_tensor(x).to(self.device, torch.float32).contiguous() for x in (k, v)), 0)
+            self.kv_set_len(layer, had)
+            return
         K, V = self.kv_views()
         n = k.shape[0]
         K[layer - 1, :, :n, :] = torch.as_tensor(k).permute(1, 0, 2).to(K.device).to(K.dtype)
@@ -271,10 +301,38 @@ class Model:
 
     def kv_read(self, layer: int, n: int):
         """Positions [0, n) of one layer as float64 numpy arrays [n, kv heads, head_dim]."""
+        if self.kvq:
+            return tuple(x.cpu().numpy().astype(np.float64) for x in self.ad_kvq_read(layer, 0, n))
         K, V = self.kv_views()
         k = K[layer - 1, :, :n, :].float().permute(1, 0, 2).cpu().numpy().astype(np.float64)
         v = V[layer - 1, :, :, :n].float().permute(2, 0, 1).cpu().numpy().astype(np.float64)
         return k, v
+
+    # ---- 8-bit cache by itself (device tensors in, device tensors out) ----
+    def ad_kvq_append(self, layer: int, k, v, pos0: int) -> None:
+        """Rotated keys and values, float32 [n, kv heads, head_dim], as positions pos0 .. of a layer whose cache ends there."""
+        s, torch = self.shape, self.torch
+        for x in (k, v):
+            assert x.dtype == torch.float32 and x.is_contiguous() and x.device == self.device
+            assert x.shape == (k.shape[0], s.n_kv_heads, s.head_dim)
+        _check(self.L.ad_kvq_append(self.model, self.kv, layer, k.data_ptr(), v.data_ptr(), s.d_kv, pos0, k.shape[0], _stream_ptr(torch)))
+
+    def ad_kvq_read(self, layer: int, pos0: int, n: int):
+        """The values of positions pos0 .. pos0 + n - 1 of a layer: (k, v), float32 [n, kv heads, head_dim]."""
+        s, torch = self.shape, self.torch
+        k, v = (torch.empty((n, s.n_kv_heads, s.head_dim), dtype=torch.float32, device=self.device) for _ in range(2))
+        _check(self.L.ad_kvq_read(self.model, self.kv, layer, pos0, n, k.data_ptr(), v.data_ptr(), s.d_kv, _stream_ptr(torch)))
+        return k, v
+
+    def ad_kvq_attend(self, layer: int, q, pos: Sequence[int]):
+        """Attention of rotated queries, float32 [m, query heads, head_dim], row r over positions 0 .. pos[r]: float32 [m, query heads * head_dim]."""
+        s, torch = self.shape, self.torch
+        p = np.ascontiguousarray(pos, dtype=np.int32)
+        assert q.dtype == torch.float32 and q.is_contiguous() and q.device == self.device
+        assert q.shape == (p.size, s.n_q_heads, s.head_dim)
+        out = torch.empty((p.size, s.d_q), dtype=torch.float32, device=self.device)
+        _check(self.L.ad_kvq_attend(self.model, self.kv, layer, q.data_ptr(), p.ctypes.data, p.size, out.data_ptr(), _stream_ptr(torch)))
+        return out
 
     # ---- steps (device tensors in, device tensors out) ----
     def ad_embed(self, tokens: Sequence[int]):

@@ -14,6 +14,7 @@
 
 #include "../../include/adadecode.h"
 #include "ad_internal.h"
+#include "ad_kvq.h"
 #include "ad_prompt.h"
 #include "ad_sched.h"
 
@@ -174,6 +175,7 @@ struct ad_model {
 struct ad_kv {
     const ad_model *model;
     char *storage;
+    bool q8;              // 8-bit entries (ad_kvq.h); half_bytes is not used then
     size_t layer_bytes, half_bytes;
     float *rope;          // [stride][dh/2][2]
     int32_t stride;       // max_pos rounded up to 64: positions per (head, dim) row of V, rows per head of K
@@ -184,7 +186,11 @@ struct ad_kv {
     // [rows][d] and their 1 / rms, activation tiles of d, dq (queries, attention output) and f inputs, fp32 pieces of the projections
     // pieces of q/k/v and of Wo may run on into Bg, which nobody holds then, those of down start at Q (nor Q, Bo then): the more pieces
     // fit, the more workgroups a short prompt's projections have
-    struct Prompt { int32_t rows; float *x, *scale, *pieces, *down_pieces; size_t pieces_floats, down_floats; char *Bd, *Q, *Bo, *Bg; } pr;
+    // 8-bit cache: rows of keys and values before they are stored, and a layer's values in bf16
+    struct Prompt { int32_t rows; float *x, *scale, *pieces, *down_pieces; size_t pieces_floats, down_floats; char *Bd, *Q, *Bo, *Bg;
+                    float *k_rows, *v_rows; uint16_t *K16, *V16; } pr;
+
+    KvqCache cache8(int32_t layer) const;
 };
 
 extern "C" {
@@ -329,16 +335,24 @@ static bool max_pos_ok(const ad_config &c, int32_t max_pos) {
     return ((int64_t)max_pos + 63) / 64 * 64 * c.head_dim <= (int64_t)1 << 31;
 }
 
-// What a cache cannot do without: the entries, the attention partials, the rotary table.
-static size_t kv_core_bytes(const ad_config &c, int32_t max_pos) {
-    const size_t elem = c.dtype == AD_F32 ? 4 : 2;
+static size_t kvq_part_bytes(const ad_config &c, int32_t max_pos) {
+    return align_up((size_t)c.n_q_heads * 8 * kvq_max_splits(max_pos) * (c.head_dim + 2) * 4);
+}
+
+static size_t kv_layer_bytes(const ad_config &c, int32_t max_pos, bool q8) {
     const size_t stride = ((size_t)max_pos + 63) / 64 * 64;
-    const size_t cache = (size_t)c.n_layers * 2 * c.n_kv_heads * stride * c.head_dim * elem;
-    return align_up(cache) + attn_part_bytes(c, max_pos) + rope_table_bytes(c, max_pos);
+    if (q8) return kvq_layer_bytes(c.n_kv_heads, (int64_t)stride, c.head_dim);
+    return (size_t)2 * c.n_kv_heads * stride * c.head_dim * (c.dtype == AD_F32 ? 4 : 2);
+}
+
+// What a cache cannot do without: the entries, the attention partials, the rotary table.
+static size_t kv_core_bytes(const ad_config &c, int32_t max_pos, bool q8) {
+    const size_t cache = (size_t)c.n_layers * kv_layer_bytes(c, max_pos, q8);
+    return align_up(cache) + (q8 ? kvq_part_bytes(c, max_pos) : attn_part_bytes(c, max_pos)) + rope_table_bytes(c, max_pos);
 }
 
 // Lays the prompt pass's scratch out from `base` (null: sizes only); returns its size.  16-bit models only.
-static size_t prompt_layout(const ad_config &c, int32_t max_pos, char *base, ad_kv::Prompt *pr) {
+static size_t prompt_layout(const ad_config &c, int32_t max_pos, bool q8, char *base, ad_kv::Prompt *pr) {
     ad_kv::Prompt p;
     memset(&p, 0, sizeof p);
     size_t off = 0;
@@ -369,35 +383,46 @@ static size_t prompt_layout(const ad_config &c, int32_t max_pos, char *base, ad_
         p.pieces_floats = (off - pieces_off) / 4;
         p.Bg = take(prompt_act_bytes(p.rows, L.f));
         if (L.f % 32 == 0) p.pieces_floats = (off - pieces_off) / 4;      // (else Bg's last tile has zeros that must stay)
+        if (q8) {
+            const size_t half = (size_t)c.n_kv_heads * (((size_t)max_pos + 63) / 64 * 64) * c.head_dim;
+            p.k_rows = (float *)take((size_t)p.rows * L.dkv * 4);
+            p.v_rows = (float *)take((size_t)p.rows * L.dkv * 4);
+            p.K16 = (uint16_t *)take(half * 2);
+            p.V16 = (uint16_t *)take(half * 2);
+        }
     }
     if (pr) *pr = p;
     return off;
 }
 
-size_t ad_kv_bytes(const ad_config *cfg, int32_t max_pos) {
+static size_t kv_bytes(const ad_config *cfg, int32_t max_pos, bool q8, const char *who) {
     const char *why;
-    if (!config_ok(cfg, &why) || max_pos < 1) { fail(AD_EINVAL, "ad_kv_bytes: %s", max_pos < 1 ? "max_pos < 1" : why); return 0; }
-    if (!max_pos_ok(*cfg, max_pos)) { fail(AD_ERANGE, "ad_kv_bytes: max_pos %d is more positions than a cache can have", max_pos); return 0; }
-    return kv_core_bytes(*cfg, max_pos) + prompt_layout(*cfg, max_pos, nullptr, nullptr);
+    if (!config_ok(cfg, &why) || max_pos < 1) { fail(AD_EINVAL, "%s: %s", who, max_pos < 1 ? "max_pos < 1" : why); return 0; }
+    if (!max_pos_ok(*cfg, max_pos)) { fail(AD_ERANGE, "%s: max_pos %d is more positions than a cache can have", who, max_pos); return 0; }
+    return kv_core_bytes(*cfg, max_pos, q8) + prompt_layout(*cfg, max_pos, q8, nullptr, nullptr);
 }
 
-ad_status ad_kv_create(const ad_model *model, void *kv_storage, size_t kv_storage_bytes, int32_t max_pos, void *stream, ad_kv **out) {
-    if (!model || !kv_storage || !out || max_pos < 1) return (ad_status)fail(AD_EINVAL, "ad_kv_create: bad argument");
-    if (((uintptr_t)kv_storage & 255u) != 0) return (ad_status)fail(AD_EINVAL, "ad_kv_create: storage must be 256-byte aligned");
-    if (!max_pos_ok(model->cfg, max_pos)) return (ad_status)fail(AD_ERANGE, "ad_kv_create: max_pos %d is more positions than a cache can have", max_pos);
-    const size_t need = kv_core_bytes(model->cfg, max_pos);
-    if (kv_storage_bytes < need) return (ad_status)fail(AD_ENOMEM, "ad_kv_create: storage has %zu bytes, %zu needed", kv_storage_bytes, need);
+size_t ad_kv_bytes(const ad_config *cfg, int32_t max_pos) { return kv_bytes(cfg, max_pos, false, "ad_kv_bytes"); }
+size_t ad_kvq_bytes(const ad_config *cfg, int32_t max_pos) { return kv_bytes(cfg, max_pos, true, "ad_kvq_bytes"); }
+
+static int kv_create(const ad_model *model, void *kv_storage, size_t kv_storage_bytes, int32_t max_pos, bool q8, void *stream, ad_kv **out,
+                     const char *who) {
+    if (!model || !kv_storage || !out || max_pos < 1) return fail(AD_EINVAL, "%s: bad argument", who);
+    if (((uintptr_t)kv_storage & 255u) != 0) return fail(AD_EINVAL, "%s: storage must be 256-byte aligned", who);
+    if (!max_pos_ok(model->cfg, max_pos)) return fail(AD_ERANGE, "%s: max_pos %d is more positions than a cache can have", who, max_pos);
+    const size_t need = kv_core_bytes(model->cfg, max_pos, q8);
+    if (kv_storage_bytes < need) return fail(AD_ENOMEM, "%s: storage has %zu bytes, %zu needed", who, kv_storage_bytes, need);
     ad_kv *kv = new (std::nothrow) ad_kv();
-    if (!kv) return (ad_status)fail(AD_ENOMEM, "ad_kv_create: out of host memory");
+    if (!kv) return fail(AD_ENOMEM, "%s: out of host memory", who);
     const ad_config &c = model->cfg;
-    const size_t elem = c.dtype == AD_F32 ? 4 : 2;
     kv->model = model;
     kv->storage = (char *)kv_storage;
+    kv->q8 = q8;
     kv->stride = (max_pos + 63) / 64 * 64;
-    kv->half_bytes = (size_t)c.n_kv_heads * (size_t)kv->stride * c.head_dim * elem;
-    kv->layer_bytes = 2 * kv->half_bytes;
+    kv->layer_bytes = kv_layer_bytes(c, max_pos, q8);
+    kv->half_bytes = kv->layer_bytes / 2;
     kv->part = (float *)(kv->storage + align_up((size_t)c.n_layers * kv->layer_bytes));
-    kv->rope = (float *)((char *)kv->part + attn_part_bytes(c, max_pos));
+    kv->rope = (float *)((char *)kv->part + (q8 ? kvq_part_bytes(c, max_pos) : attn_part_bytes(c, max_pos)));
     kv->max_pos = max_pos;
     kv->len.assign(c.n_layers, 0);
     // rotary table for every position of this cache; frequencies base^(-2i/dh) in double
@@ -407,9 +432,9 @@ ad_status ad_kv_create(const ad_model *model, void *kv_storage, size_t kv_storag
     int rc = launch_rope_table(ra, stream);
     // storage without room for the prompt pass's scratch is a cache all the same: prompts then go through in layer steps
     memset(&kv->pr, 0, sizeof kv->pr);
-    const size_t prompt_bytes = prompt_layout(c, max_pos, nullptr, nullptr);
+    const size_t prompt_bytes = prompt_layout(c, max_pos, q8, nullptr, nullptr);
     if (!rc && prompt_bytes && kv_storage_bytes >= need + prompt_bytes) {
-        prompt_layout(c, max_pos, kv->storage + need, &kv->pr);
+        prompt_layout(c, max_pos, q8, kv->storage + need, &kv->pr);
         // all of it is written before it is read, but for the inputs that fill the last operand tile of a width that is no
         // multiple of 32: the weights have zeros there, and so must the activations have (zero times NaN is NaN)
         const Layout &L = model->lay;
@@ -417,9 +442,16 @@ ad_status ad_kv_create(const ad_model *model, void *kv_storage, size_t kv_storag
         if (!rc && L.f % 32) rc = launch_zero(kv->pr.Bg, prompt_act_bytes(kv->pr.rows, L.f), stream);
     }
     if (!rc) rc = stream_sync(stream);
-    if (rc) { delete kv; return (ad_status)hip_fail(rc, "ad_kv_create: rotary table"); }
+    if (rc) { delete kv; return hip_fail(rc, who); }
     *out = kv;
     return AD_OK;
+}
+
+ad_status ad_kv_create(const ad_model *model, void *kv_storage, size_t kv_storage_bytes, int32_t max_pos, void *stream, ad_kv **out) {
+    return (ad_status)kv_create(model, kv_storage, kv_storage_bytes, max_pos, false, stream, out, "ad_kv_create");
+}
+ad_status ad_kvq_create(const ad_model *model, void *kv_storage, size_t kv_storage_bytes, int32_t max_pos, void *stream, ad_kv **out) {
+    return (ad_status)kv_create(model, kv_storage, kv_storage_bytes, max_pos, true, stream, out, "ad_kvq_create");
 }
 
 ad_status ad_kv_destroy(ad_kv *kv) { delete kv; return AD_OK; }
@@ -514,11 +546,16 @@ static int fused_health(const ad_model *m, void *stream) {
                             "invalid (take the cache back to its length before that call)");
 }
 
-static int64_t layer_step_bytes(const ad_config &c, int32_t ctx, int32_t m) {
+static int64_t kv_position_bytes(const ad_config &c, bool q8) {       // K and V of one position of a layer
+    if (q8) return 2 * (int64_t)c.n_kv_heads * (c.head_dim + 1);
+    return 2 * (int64_t)c.n_kv_heads * c.head_dim * (c.dtype == AD_F32 ? 4 : 2);
+}
+
+static int64_t layer_step_bytes(const ad_config &c, int32_t ctx, int32_t m, bool q8) {
     const int64_t s = c.dtype == AD_F32 ? 4 : 2;
     const int64_t dq = (int64_t)c.n_q_heads * c.head_dim, dkv = (int64_t)c.n_kv_heads * c.head_dim, d = c.d_model, f = c.d_ffn;
     const int64_t w = ((dq + 2 * dkv) * d + d * dq + 3 * d * f) * s;
-    return w + 2 * dkv * s * ((int64_t)ctx + m) + 2 * dkv * s * m;
+    return w + kv_position_bytes(c, q8) * ((int64_t)ctx + 2 * m);
 }
 
 // Step 1 of a layer: q, k, v = W (RMSNorm(x)).  The norm is fused into the GEMM (B operand built from x in its
@@ -546,6 +583,11 @@ static int qkv_ahead(const ad_model *m, int32_t layer, const void *hidden, int32
     return rc ? hip_fail(rc, "layer step: qkv issued ahead") : AD_OK;
 }
 
+KvqCache ad_kv::cache8(int32_t layer) const {
+    return kvq_cache(storage + (size_t)(layer - 1) * layer_bytes, stride, model->cfg.n_kv_heads, model->cfg.head_dim);
+}
+static float attn8_scale(int dh) { return 1.44269504088896341f / sqrtf((float)dh); }       // log2(e) / sqrt(dh)
+
 // Layers layer .. layer + count - 1 over the same rows.  The fused mode runs them in one launch (the layers' weights
 // and caches are laid out at a constant distance from one layer to the next); otherwise one layer at a time.
 static int layer_steps(const ad_model *m, ad_kv *kv, int32_t layer, int32_t count, void *hidden, const int32_t *pos, int32_t n,
@@ -565,6 +607,7 @@ static int layer_steps(const ad_model *m, ad_kv *kv, int32_t layer, int32_t coun
     const LaunchCtx ctx = launch_ctx(m, stream);
     const int ek = elem_kind(c);
     const bool fused = m->layer_mode == AD_LAYER_FUSED;
+    if (fused && kv->q8) return fail(AD_ESTATE, "%s: the fused layer step does not run on an 8-bit cache", who);
     int rc;
     // The arguments of layer ly's five steps.  from_prev: the layer before it ran in this same call and its down
     // projection left this layer's QKV input behind (see step 5); feeds_next: this layer's down projection does
@@ -609,12 +652,28 @@ static int layer_steps(const ad_model *m, ad_kv *kv, int32_t layer, int32_t coun
         }
     };
 
+    // step 2 over an 8-bit cache: rotation and append are a kernel of their own, attention reads every row from the cache
+    auto attn8 = [&](int32_t ly) {
+        KvqRotate r;
+        r.c = kv->cache8(ly); r.qkv = m->qkv; r.ld = L.nqkv; r.m = n; r.Hq = c.n_q_heads; r.pos0 = pos[0]; r.rope = a.rope;
+        const int e = launch_kvq_rotate(r, ctx);
+        if (e) return e;
+        KvqAttn at;
+        memset(&at, 0, sizeof at);
+        at.c = r.c; at.q = m->qkv; at.ld_q = L.nqkv; at.m = n; at.Hq = c.n_q_heads;
+        for (int i = 0; i < n; ++i) at.see[i] = pos[i];
+        at.scale = attn8_scale(L.dh); at.part = kv->part; at.Bo = m->Bo; at.Bo_KT = L.kt_q; at.f16 = ek == kElemF16;
+        kvq_attn_finish(at, m->n_wg);
+        return launch_kvq_attn(at, ctx);
+    };
+
     if (!fused) {
         // one kernel per phase, layer after layer
         for (int32_t ly = layer; ly < layer + count; ++ly) {
             build(ly, ly > layer, ly + 1 < layer + count);
             if (!(first_qkv_issued && ly == layer) && (rc = gemm(m, gq, L.nqkv, L.d, ctx))) return hip_fail(rc, "layer step: qkv");
-            if ((rc = launch_attn(a, ctx))) return hip_fail(rc, "layer step: attention");
+            rc = kv->q8 ? attn8(ly) : launch_attn(a, ctx);
+            if (rc) return hip_fail(rc, "layer step: attention");
             if ((rc = gemm(m, go, L.d, L.dq, ctx))) return hip_fail(rc, "layer step: wo");
             if ((rc = gemm(m, gg, 2 * (int64_t)L.f, L.d, ctx))) return hip_fail(rc, "layer step: gate/up");
             if ((rc = gemm(m, gd, L.d, L.f, ctx))) return hip_fail(rc, "layer step: down");
@@ -645,7 +704,7 @@ static int layer_steps(const ad_model *m, ad_kv *kv, int32_t layer, int32_t coun
         f.nwg_gu = fused_phase_workgroups(gg.NT, m->n_wg);
         f.nwg_down = fused_phase_workgroups(gd.NT, m->n_wg);
         f.ctr = m->bar_ctr; f.round0 = m->bar_round; f.abort_flag = m->bar_abort; f.trace = m->layer_trace;
-        const bool sample = profile_begin(m->prof, AD_PROF_LAYER, count * layer_step_bytes(c, pos[0], n), stream);
+        const bool sample = profile_begin(m->prof, AD_PROF_LAYER, count * layer_step_bytes(c, pos[0], n, kv->q8), stream);
         rc = launch_layer_fused(f, ctx);
         if (sample) (void)event_record(m->prof.stop.back(), stream);
         if (rc) return hip_fail(rc, "layer step: fused kernel");
@@ -664,6 +723,67 @@ ad_status ad_layer_steps(const ad_model *m, ad_kv *kv, int32_t first_layer, int3
     return (ad_status)layer_steps(m, kv, first_layer, n_layers, hidden, pos, n, stream, "ad_layer_steps");
 }
 
+// ---- 8-bit cache by itself ---------------------------------------------------------------------------
+static int kvq_args(const ad_model *m, const ad_kv *kv, int32_t layer, const char *who) {
+    if (kv->model != m) return fail(AD_EINVAL, "%s: cache belongs to another model", who);
+    if (!kv->q8) return fail(AD_ESTATE, "%s: not an 8-bit cache", who);
+    if (layer < 1 || layer > m->cfg.n_layers) return fail(AD_ERANGE, "%s: layer %d outside 1..%d", who, layer, m->cfg.n_layers);
+    return AD_OK;
+}
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+ad_status ad_kvq_append(const ad_model *m, ad_kv *kv, int32_t layer, const void *k, const void *v, int64_t ld, int32_t pos0, int32_t n, void *stream) {
+    if (!m || !kv || !k || !v) return (ad_status)fail(AD_EINVAL, "ad_kvq_append: null argument");
+    int rc = kvq_args(m, kv, layer, "ad_kvq_append");
+    if (rc) return (ad_status)rc;
+    if (!aligned16(k) || !aligned16(v) || ld < m->lay.dkv || ld % 4)
+        return (ad_status)fail(AD_EINVAL, "ad_kvq_append: rows must be 16-byte aligned and at least n_kv_heads * head_dim apart");
+    if (n < 1 || pos0 < 0 || n > kv->max_pos - pos0)
+        return (ad_status)fail(AD_ERANGE, "ad_kvq_append: %d rows from position %d on do not fit max_pos %d", n, pos0, kv->max_pos);
+    if (pos0 != kv->len[layer - 1]) return (ad_status)fail(AD_ESTATE, "ad_kvq_append: pos0 = %d but layer %d's cache ends at %d", pos0, layer, kv->len[layer - 1]);
+    KvqRows a;
+    memset(&a, 0, sizeof a);
+    a.c = kv->cache8(layer); a.k = (const float *)k; a.v = (const float *)v; a.ld = ld; a.n = n; a.pos0 = pos0;
+    if ((rc = launch_kvq_store(a, launch_ctx(m, stream)))) return (ad_status)hip_fail(rc, "ad_kvq_append");
+    kv->len[layer - 1] += n;
+    return AD_OK;
+}
+
+ad_status ad_kvq_read(const ad_model *m, const ad_kv *kv, int32_t layer, int32_t pos0, int32_t n, void *k, void *v, int64_t ld, void *stream) {
+    if (!m || !kv || !k || !v) return (ad_status)fail(AD_EINVAL, "ad_kvq_read: null argument");
+    int rc = kvq_args(m, kv, layer, "ad_kvq_read");
+    if (rc) return (ad_status)rc;
+    if (!aligned16(k) || !aligned16(v) || ld < m->lay.dkv || ld % 4)
+        return (ad_status)fail(AD_EINVAL, "ad_kvq_read: rows must be 16-byte aligned and at least n_kv_heads * head_dim apart");
+    if (n < 1 || pos0 < 0 || n > kv->len[layer - 1] - pos0)
+        return (ad_status)fail(AD_ERANGE, "ad_kvq_read: positions %d .. %lld of a cache that ends at %d", pos0, (long long)pos0 + n - 1, kv->len[layer - 1]);
+    KvqRows a;
+    memset(&a, 0, sizeof a);
+    a.c = kv->cache8(layer); a.k_out = (float *)k; a.v_out = (float *)v; a.ld = ld; a.n = n; a.pos0 = pos0;
+    rc = launch_kvq_read(a, launch_ctx(m, stream));
+    return rc ? (ad_status)hip_fail(rc, "ad_kvq_read") : AD_OK;
+}
+
+ad_status ad_kvq_attend(const ad_model *m, const ad_kv *kv, int32_t layer, const void *q, const int32_t *pos, int32_t n, void *out, void *stream) {
+    if (!m || !kv || !q || !pos || !out) return (ad_status)fail(AD_EINVAL, "ad_kvq_attend: null argument");
+    int rc = kvq_args(m, kv, layer, "ad_kvq_attend");
+    if (rc) return (ad_status)rc;
+    if (!aligned16(q) || !aligned16(out)) return (ad_status)fail(AD_EINVAL, "ad_kvq_attend: rows must be 16-byte aligned");
+    if (n < 1 || n > m->cfg.m_max) return (ad_status)fail(AD_ERANGE, "ad_kvq_attend: m = %d outside 1..%d", n, m->cfg.m_max);
+    KvqAttn a;
+    memset(&a, 0, sizeof a);
+    for (int i = 0; i < n; ++i) {
+        if (pos[i] < 0 || pos[i] >= kv->len[layer - 1])
+            return (ad_status)fail(AD_ERANGE, "ad_kvq_attend: position %d of a cache that ends at %d", pos[i], kv->len[layer - 1]);
+        a.see[i] = pos[i];
+    }
+    a.c = kv->cache8(layer); a.q = (const float *)q; a.ld_q = m->lay.dq; a.m = n; a.Hq = m->cfg.n_q_heads;
+    a.scale = attn8_scale(m->lay.dh); a.part = kv->part; a.out = (float *)out;
+    kvq_attn_finish(a, m->n_wg);
+    rc = launch_kvq_attn(a, launch_ctx(m, stream));
+    return rc ? (ad_status)hip_fail(rc, "ad_kvq_attend") : AD_OK;
+}
+
 // The prompt pass over n <= kv->pr.rows tokens at positions pos0 .. (pos0 a multiple of 64): fills every layer's cache.  The
 // rows' hidden states after the last layer are needed by nobody (the prompt's last token is not part of the pass), so
 // the last layer ends with its K and V.
@@ -671,6 +791,7 @@ static int prompt_pass(const ad_model *m, ad_kv *kv, const int32_t *tokens, int3
     const ad_config &c = m->cfg;
     const Layout &L = m->lay;
     const int ek = elem_kind(c), f16 = ek == kElemF16;
+    const LaunchCtx ctx = launch_ctx(m, stream);
     int rc;
     PromptEmbed e;
     e.table = m->embed; e.elem = ek; e.d = L.d;
@@ -704,13 +825,27 @@ static int prompt_pass(const ad_model *m, ad_kv *kv, const int32_t *tokens, int3
         q.part = kv->pr.pieces; q.scale = kv->pr.scale; q.M = n; q.Hq = c.n_q_heads; q.Hkv = c.n_kv_heads; q.dh = L.dh; q.G = c.n_q_heads / c.n_kv_heads;
         q.rope = kv->rope + (size_t)pos0 * (L.dh / 2) * 2;
         q.Kc = kv->storage + (size_t)l * kv->layer_bytes; q.Vc = (char *)q.Kc + kv->half_bytes;
-        q.stride = kv->stride; q.pos0 = pos0; q.q_rows = kv->pr.rows * q.G; q.Q = kv->pr.Q; q.q_scale = 1.0f / sqrtf((float)L.dh); q.f16 = f16;
+        q.stride = kv->stride; q.pos0 = pos0; q.q_rows = kv->pr.rows * q.G; q.Q = kv->pr.Q; q.q_scale = 1.0f / sqrtf((float)L.dh); q.f16 = kv->q8 ? 0 : f16;
+        q.k_rows = kv->pr.k_rows; q.v_rows = kv->pr.v_rows;
         if ((rc = launch_prompt_qkv(q, stream))) return hip_fail(rc, "prompt pass: rotation");
+        if (kv->q8) {
+            KvqRows st;
+            memset(&st, 0, sizeof st);
+            st.c = kv->cache8(l + 1); st.k = q.k_rows; st.v = q.v_rows; st.ld = L.dkv; st.n = n; st.pos0 = pos0;
+            if ((rc = launch_kvq_store(st, ctx))) return hip_fail(rc, "prompt pass: store");
+        }
         if (last) break;
+        if (kv->q8) {
+            // the attention kernel reads 16-bit entries: the layer's values, which bf16 holds exactly
+            KvqExpand x;
+            x.c = kv->cache8(l + 1); x.K = kv->pr.K16; x.V = kv->pr.V16; x.n = pos0 + n;
+            if ((rc = launch_kvq_expand(x, ctx))) return hip_fail(rc, "prompt pass: values");
+            q.Kc = x.K; q.Vc = x.V;
+        }
         PromptAttn a;
         memset(&a, 0, sizeof a);
         a.Q = kv->pr.Q; a.Kc = q.Kc; a.Vc = q.Vc; a.stride = kv->stride; a.pos0 = pos0; a.M = n; a.Hq = q.Hq; a.Hkv = q.Hkv; a.dh = L.dh; a.G = q.G;
-        a.q_rows = q.q_rows; a.Bo = kv->pr.Bo; a.Bo_KT = L.kt_q; a.f16 = f16;
+        a.q_rows = q.q_rows; a.Bo = kv->pr.Bo; a.Bo_KT = L.kt_q; a.f16 = q.f16; a.f16_out = f16;
         if ((rc = launch_prompt_attn(a, stream))) return hip_fail(rc, "prompt pass: attention");
         if ((rc = project(lp.wo, kv->pr.Bo, L.kt_q, L.d, &rows.n_split, kv->pr.pieces, kv->pr.pieces_floats))) return hip_fail(rc, "prompt pass: wo");
         rows.part = kv->pr.pieces;
@@ -974,7 +1109,7 @@ ad_status ad_probe_stream(const ad_model *m, const ad_kv *kv, int32_t layer, int
     const char *cache = (const char *)kv->storage + (size_t)(layer - 1) * kv->layer_bytes;
     // as many bytes of the layer's cache as ctx positions of K and V hold (the cache is position-major per head;
     // the probe reads the same number of bytes from the start of the layer's block)
-    size_t kv_bytes = 2 * (size_t)m->cfg.n_kv_heads * m->cfg.head_dim * (m->cfg.dtype == AD_F32 ? 4 : 2) * (size_t)ctx;
+    size_t kv_bytes = (size_t)kv_position_bytes(m->cfg, kv->q8) * (size_t)ctx;
     kv_bytes = (kv_bytes < kv->layer_bytes ? kv_bytes : kv->layer_bytes) & ~(size_t)15;
     unsigned *sink = m->bar_ctr + 24;       // a word of the model's scratch that nothing reads; the probe never writes it
     int rc;
@@ -1049,7 +1184,7 @@ struct GpuBackend : Backend {
     int layer_step(int32_t layer, int32_t row0, int32_t n, int32_t pos0) override { return layer_steps(layer, 1, row0, n, pos0); }
     int layer_steps(int32_t first_layer, int32_t count, int32_t row0, int32_t n, int32_t pos0) override {
         for (int i = 0; i < n; ++i) pos_buf[i] = pos0 + i;
-        if (!in_prefill) bytes += count * layer_step_bytes(m->cfg, pos0, n);
+        if (!in_prefill) bytes += count * layer_step_bytes(m->cfg, pos0, n, kv->q8);
         // the step's QKV projection may already be on the stream
         const bool qkv_there = issued.kind != AHEAD_NONE && issued.layer == first_layer && issued.row0 == row0 && issued.m == n &&
                                (issued.kind == AHEAD_LAYER || embed_taken) && m->layer_mode == AD_LAYER_KERNELS;

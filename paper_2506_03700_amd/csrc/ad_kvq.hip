@@ -1,0 +1,677 @@
+// The 8-bit cache: storing key and value rows, reading them out, and attention over them (layout: ad_kvq.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ad_device.h"
+#include "ad_internal.h"
+#include "ad_kvq.h"
+#include "ad_launch.h"
+
+namespace ad {
+
+namespace {
+
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+
+// ---------------------------------------------------------------------------------------------------
+// quantisation
+// ---------------------------------------------------------------------------------------------------
+// The exponent byte of a row whose largest magnitude is amax: e the smallest with amax <= 448 * 2^e (448 = 1.75 * 2^8 is the largest code), not
+// below -126, where 2^e and 2^-e are both normal numbers.
+__device__ __forceinline__ uint32_t scale_byte(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int b = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (uint32_t)(b < 1 ? 1 : b);
+}
+__device__ __forceinline__ float two_to(uint32_t byte) { return __uint_as_float(byte << 23); }             // the scale itself
+__device__ __forceinline__ float two_to_minus(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+// magnitude for the scale: entries that are infinite or not numbers have no part in it
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;
+}
+// codes of four values already divided by the scale: rounded to nearest even by the conversion (within range by the choice of the scale);
+// the code that is not a number for entries that are not finite
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+    auto one = [](float x) { return fabsf(x) <= 448.f ? x : 0.f; };
+    uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(one(a), one(b), 0, false);
+    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(one(c), one(d), (int)w, true);
+    if (!(fabsf(a) <= 448.f)) w = (w & ~0xffu) | 0x7fu;
+    if (!(fabsf(b) <= 448.f)) w = (w & ~0xff00u) | 0x7f00u;
+    if (!(fabsf(c) <= 448.f)) w = (w & ~0xff0000u) | 0x7f0000u;
+    if (!(fabsf(d) <= 448.f)) w = (w & ~0xff000000u) | 0x7f000000u;
+    return w;
+}
+__device__ __forceinline__ uint8_t code1(float x) { return (uint8_t)(codes4(x, 0.f, 0.f, 0.f) & 0xffu); }
+// largest value over N = 8 or 16 neighbouring lanes
+template <int N>
+__device__ __forceinline__ float max_lanes(float v) {
+    v = fmaxf(v, dpp<0xB1>(v));
+    v = fmaxf(v, dpp<0x4E>(v));
+    v = fmaxf(v, dpp<0x141>(v));
+    if (N == 16) v = fmaxf(v, dpp<0x140>(v));
+    return v;
+}
+template <int SEL>
+__device__ __forceinline__ f32x2 values2(uint32_t w) {
+    const auto v = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, SEL);
+    return (f32x2){v[0], v[1]};
+}
+
+// ---------------------------------------------------------------------------------------------------
+// store and read-out: a workgroup per block of 64 positions and kv head
+// ---------------------------------------------------------------------------------------------------
+// DH / 8 lanes hold a row, 8 entries each, so a wavefront reads 2 KiB of consecutive entries of 4 (8) rows at a time and the largest magnitude
+// is a matter of three (four) moves between lanes.  K rows are stored as they are; V goes through LDS, so that a block of 64 positions that is stored
+// whole leaves in 16-byte pieces.
+template <int DH>
+__global__ void __launch_bounds__(256) k_kvq_store(KvqRows a) {
+    constexpr int LR = DH / 8, RP = 256 / LR;
+    __shared__ __attribute__((aligned(16))) uint8_t vt[DH][kKvqBlock + 16];
+    const int tid = threadIdx.x, g = blockIdx.y, p0 = (a.pos0 / kKvqBlock + (int)blockIdx.x) * kKvqBlock;
+    const int first = p0 > a.pos0 ? p0 : a.pos0, last = a.pos0 + a.n;
+    const int end = p0 + kKvqBlock < last ? p0 + kKvqBlock : last;
+    const int d = tid % LR * 8;
+    const KvqCache &c = a.c;
+    for (int p = first + tid / LR; p < end; p += RP) {
+        const size_t at = (size_t)(p - a.pos0) * a.ld + g * DH + d;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const float *src = (kv ? a.v : a.k) + at;
+            const f32x4 x = *(const f32x4 *)src, y = *(const f32x4 *)(src + 4);
+            float m = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(finite_abs(x[e]), finite_abs(y[e])));
+            const uint32_t b = scale_byte(max_lanes<LR>(m));
+            const float mul = two_to_minus(b);
+            const u32x2 w = {codes4(x[0] * mul, x[1] * mul, x[2] * mul, x[3] * mul), codes4(y[0] * mul, y[1] * mul, y[2] * mul, y[3] * mul)};
+            if (d == 0) (kv ? c.Vs : c.Ks)[(size_t)g * c.stride + p] = (uint8_t)b;
+            if (kv == 0) {
+                *(u32x2 *)(c.Kc + ((size_t)g * c.stride + p) * DH + d) = w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) vt[d + e][p - p0] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+            }
+        }
+    }
+    __syncthreads();
+    uint8_t *V = c.Vc + ((size_t)g * c.stride + p0) * DH;
+    if (first == p0 && end == p0 + kKvqBlock) {
+        for (int i = tid; i < DH * 4; i += 256) *(u32x4 *)(V + i * 16) = *(const u32x4 *)&vt[i >> 2][(i & 3) * 16];
+    } else {
+        const int n = end - first;
+        for (int i = tid; i < DH * n; i += 256) {
+            const int e = i / n, p = first - p0 + i % n;
+            V[e * kKvqBlock + p] = vt[e][p];
+        }
+    }
+}
+
+template <int DH>
+__global__ void __launch_bounds__(256) k_kvq_read(KvqRows a) {
+    constexpr int LR = DH / 8, RP = 256 / LR;
+    __shared__ __attribute__((aligned(16))) uint8_t vt[DH][kKvqBlock + 16];
+    const int tid = threadIdx.x, g = blockIdx.y, p0 = (a.pos0 / kKvqBlock + (int)blockIdx.x) * kKvqBlock;
+    const int first = p0 > a.pos0 ? p0 : a.pos0, last = a.pos0 + a.n;
+    const int end = p0 + kKvqBlock < last ? p0 + kKvqBlock : last;
+    const int d = tid % LR * 8;
+    const KvqCache &c = a.c;
+    const uint8_t *V = c.Vc + ((size_t)g * c.stride + p0) * DH;
+    for (int i = tid; i < DH * 4; i += 256) *(u32x4 *)&vt[i >> 2][(i & 3) * 16] = *(const u32x4 *)(V + i * 16);
+    __syncthreads();
+    for (int p = first + tid / LR; p < end; p += RP) {
+        const size_t at = (size_t)(p - a.pos0) * a.ld + g * DH + d, row = (size_t)g * c.stride + p;
+        auto put = [&](float *dst, u32x2 w, float s) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x2 lo = values2<0>(w[h]), hi = values2<1>(w[h]);
+                *(f32x4 *)(dst + 4 * h) = (f32x4){lo[0] * s, lo[1] * s, hi[0] * s, hi[1] * s};
+            }
+        };
+        put(a.k_out + at, *(const u32x2 *)(c.Kc + row * DH + d), two_to(c.Ks[row]));
+        u32x2 w = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2] |= (uint32_t)vt[d + e][p - p0] << (8 * (e & 3));
+        put(a.v_out + at, w, two_to(c.Vs[row]));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// a layer step's rows: a wavefront per token and head, lane i has dimensions i and i + dh / 2
+// ---------------------------------------------------------------------------------------------------
+template <int DH>
+__global__ void __launch_bounds__(256) k_kvq_rotate(KvqRotate a) {
+    constexpr int half = DH / 2;
+    const int heads = a.Hq + 2 * a.c.Hkv, w = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (w >= a.m * heads) return;
+    const int t = w / heads, head = w - t * heads, i = lane & (half - 1);
+    const bool live = lane < half;
+    float *row = a.qkv + (size_t)t * a.ld + (size_t)head * DH;
+    float x = row[i], y = row[i + half];
+    if (head < a.Hq + a.c.Hkv) {
+        const float cs = a.rope[(t * half + i) * 2], sn = a.rope[(t * half + i) * 2 + 1], r0 = x * cs - y * sn, r1 = x * sn + y * cs;
+        x = r0;
+        y = r1;
+        if (head < a.Hq) {
+            if (live) {
+                row[i] = x;
+                row[i + half] = y;
+            }
+            return;
+        }
+    }
+    const bool is_v = head >= a.Hq + a.c.Hkv;
+    const int g = head - a.Hq - (is_v ? a.c.Hkv : 0), p = a.pos0 + t;
+    const uint32_t b = scale_byte(max64(fmaxf(finite_abs(x), finite_abs(y))));
+    const float mul = two_to_minus(b);
+    const uint8_t c0 = code1(x * mul), c1 = code1(y * mul);
+    if (!live) return;
+    const size_t at = (size_t)g * a.c.stride + p;
+    if (is_v) {
+        uint8_t *V = a.c.Vc + ((size_t)g * a.c.stride + (p & ~(kKvqBlock - 1))) * DH + (p & (kKvqBlock - 1));
+        V[i * kKvqBlock] = c0;
+        V[(i + half) * kKvqBlock] = c1;
+        if (i == 0) a.c.Vs[at] = (uint8_t)b;
+    } else {
+        a.c.Kc[at * DH + i] = c0;
+        a.c.Kc[at * DH + i + half] = c1;
+        if (i == 0) a.c.Ks[at] = (uint8_t)b;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// the values in bf16 for the prompt pass (exact: four significant bits and a power of two)
+// ---------------------------------------------------------------------------------------------------
+template <int DH>
+__global__ void __launch_bounds__(256) k_kvq_expand(KvqExpand a) {
+    const int tid = threadIdx.x, g = blockIdx.y, p0 = blockIdx.x * kKvqBlock;
+    const KvqCache &c = a.c;
+    __shared__ float vs[kKvqBlock];
+    if (tid < kKvqBlock) vs[tid] = p0 + tid < a.n ? two_to(c.Vs[(size_t)g * c.stride + p0 + tid]) : 0.f;
+    __syncthreads();
+    // 8 codes of a K row per thread and turn
+    for (int i = tid; i < kKvqBlock * (DH / 8); i += 256) {
+        const int p = p0 + i / (DH / 8), d = i % (DH / 8) * 8;
+        const size_t row = (size_t)g * c.stride + p;
+        u16x8 o = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (p < a.n) {
+            const u32x2 w = *(const u32x2 *)(c.Kc + row * DH + d);
+            const float s = two_to(c.Ks[row]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x2 lo = values2<0>(w[h]), hi = values2<1>(w[h]);
+                o[4 * h] = to16<false>(lo[0] * s);
+                o[4 * h + 1] = to16<false>(lo[1] * s);
+                o[4 * h + 2] = to16<false>(hi[0] * s);
+                o[4 * h + 3] = to16<false>(hi[1] * s);
+            }
+        }
+        *(u16x8 *)(a.K + row * DH + d) = o;
+    }
+    // 8 positions of a dimension
+    const uint8_t *V = c.Vc + ((size_t)g * c.stride + p0) * DH;
+    for (int i = tid; i < DH * (kKvqBlock / 8); i += 256) {
+        const int d = i / (kKvqBlock / 8), p = i % (kKvqBlock / 8) * 8;
+        const u32x2 w = *(const u32x2 *)(V + d * kKvqBlock + p);
+        u16x8 o;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x2 lo = values2<0>(w[h]), hi = values2<1>(w[h]);
+            const float x[4] = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[4 * h + e] = p0 + p + 4 * h + e < a.n ? to16<false>(x[e] * vs[p + 4 * h + e]) : (uint16_t)0;
+        }
+        *(u16x8 *)(a.V + ((size_t)g * DH + d) * c.stride + p0 + p) = o;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------------------
+// Work item (kv head, split): a workgroup of four wavefronts that take the item's blocks of 64 positions in turn, under an online softmax of their
+// own; their results meet in LDS, the items' in k_kvq_combine.  All query rows of the kv head's group meet a block's codes while they are in registers.
+//
+// Products.  S^T = K q^T: codes are exact in fp16, queries are scaled to a largest magnitude in [128, 256) and split into fp16 hi and lo parts (22 bits), sums are
+// fp32.  A lane loads 16 consecutive dimensions of a key: the first eight are its part of one k-step, the other eight of the next, and the queries are
+// dealt out the same way.  Rows of the four score tiles are assigned to keys so that lane (n, gq) ends up with keys gq * 16 .. + 15 of query row n, which is, eight by
+// eight, the B operand of O^T = V^T P^T against 16 consecutive positions of a dimension.  The scales never touch the codes: K's multiply the scores, V's the
+// probabilities, relative to the largest that the row has seen so that fp16 has them all in range (again hi and lo).
+template <int DH>
+struct KvqAttnLds {                                        // of one row tile at a time
+    float mx[kKvqWaves][16], sum[kKvqWaves][16];
+    float part[kKvqWaves][16][DH + 4];                     // (rows padded to 16 bytes for 128-bit stores)
+};
+
+// x / d for any x >= 0: the rounded-up reciprocal is never too small and, below 2^32, at most one too large
+__device__ __forceinline__ int quotient(int x, int d, unsigned mul) {
+    const int q = div_small(x, mul);
+    return q * d > x ? q - 1 : q;
+}
+
+// 8 codes as an MFMA operand
+__device__ __forceinline__ f16x8 operand(uint32_t w0, uint32_t w1) {
+    const half2_t a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, true);
+    const half2_t c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, true);
+    return (f16x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ f32x4 mma(const f16x8 &a, const f16x8 &b, const f32x4 &c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// output of query row r (of kv head g), dimensions d, d + 1
+__device__ __forceinline__ void kvq_output(const KvqAttn &a, int g, int r, int d, float y0, float y1) {
+    const int t = quotient(r, a.G, a.mul_G), col = (g * a.G + (r - t * a.G)) * a.c.dh + d;
+    if (a.out) {
+        *(f32x2 *)(a.out + (size_t)t * a.Hq * a.c.dh + col) = (f32x2){y0, y1};
+    } else if (a.f16) {
+        store_act<true>(a.Bo, a.Bo_KT, col, t, y0);
+        store_act<true>(a.Bo, a.Bo_KT, col + 1, t, y1);
+    } else {
+        store_act<false>(a.Bo, a.Bo_KT, col, t, y0);
+        store_act<false>(a.Bo, a.Bo_KT, col + 1, t, y1);
+    }
+}
+
+template <int DH, int RT>
+__global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
+    constexpr int J = DH / 64, DT = DH / 16, RP = RT * 16, PR = DH + 2;
+    constexpr int kPBits = 14;                             // probabilities times 2^14: those of 2^-17 and more keep 22 bits in fp16 hi and lo
+    __shared__ __attribute__((aligned(16))) KvqAttnLds<DH> L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, gq = lane >> 4;
+    const int item = blockIdx.x, g = quotient(item, a.S, a.mul_S), s = item - g * a.S;
+    const int b_end = (a.n + kKvqBlock - 1) / kKvqBlock, b0 = s * a.per, b1 = b0 + a.per < b_end ? b0 + a.per : b_end;
+    const uint8_t *Kg = a.c.Kc + (size_t)g * a.c.stride * DH, *Vg = a.c.Vc + (size_t)g * a.c.stride * DH;
+    const uint8_t *Ksg = a.c.Ks + (size_t)g * a.c.stride, *Vsg = a.c.Vs + (size_t)g * a.c.stride;
+
+    u32x4 k[4][J], v[DT], ks, vs;
+    auto load_k = [&](int b) {
+        const uint8_t *base = Kg + (size_t)b * kKvqBlock * DH + ((n >> 2) * 16 + (n & 3)) * DH + gq * 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < J; ++j) k[t][j] = *(const u32x4 *)(base + t * 4 * DH + j * 64);
+        ks = *(const u32x4 *)(Ksg + (size_t)b * kKvqBlock + gq * 16);
+    };
+    auto load_v = [&](int b) {
+        const uint8_t *base = Vg + (size_t)b * kKvqBlock * DH + n * kKvqBlock + gq * 16;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) v[d] = *(const u32x4 *)(base + d * 16 * kKvqBlock);
+        vs = *(const u32x4 *)(Vsg + (size_t)b * kKvqBlock + gq * 16);
+    };
+
+    for (int r0 = 0; r0 < a.R; r0 += RP) {
+        const int nr = a.R - r0 < RP ? a.R - r0 : RP;
+        int b = b0 + wave;
+        if (b < b1) {
+            load_k(b);
+            load_v(b);
+        }
+        // queries, each lane its own part; rows past the last are zeros
+        f16x8 q[RT][J][2][2];                              // [.][k-step of the pair][hi, lo]
+        float q_mul[RT], mx[RT], sum[RT];
+        int t_row[RT], see[RT], e_ref[RT];                 // o is in units of 2^(e_ref - 127 - kPBits)
+        f32x4 o[RT][DT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int rr = i * 16 + n, r = r0 + (rr < nr ? rr : 0), t = quotient(r, a.G, a.mul_G), hq = g * a.G + (r - t * a.G);
+            const float *qp = a.q + (size_t)t * a.ld_q + (size_t)hq * DH + gq * 16;
+            float x[J][16], m = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 w = *(const f32x4 *)(qp + j * 64 + e * 4);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        x[j][e * 4 + c] = rr < nr ? w[c] : 0.f;
+                        m = fmaxf(m, finite_abs(x[j][e * 4 + c]));
+                    }
+                }
+            m = max_rows(m);
+            // 2^(7 - exponent of m): both it and its inverse stay normal numbers
+            int ex = (int)(__float_as_uint(m) >> 23) - 127;
+            ex = ex < -100 ? -100 : ex;
+            const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+            q_mul[i] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale;
+            t_row[i] = t;
+            see[i] = a.see[0];
+#pragma unroll
+            for (int c = 1; c < 8; ++c) see[i] = t == c ? a.see[c] : see[i];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u16x8 hi8, lo8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        uint16_t hi, lo;
+                        split16<true>(x[j][h * 8 + e] * up, hi, lo);
+                        hi8[e] = hi;
+                        lo8[e] = lo;
+                    }
+                    q[i][j][h][0] = __builtin_bit_cast(f16x8, hi8);
+                    q[i][j][h][1] = __builtin_bit_cast(f16x8, lo8);
+                }
+            mx[i] = -INFINITY;
+            sum[i] = 0.f;
+            e_ref[i] = 0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[i][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+
+        for (; b < b1; b += kKvqWaves) {
+            const int p0 = b * kKvqBlock;
+            const bool part_hidden = p0 + kKvqBlock > a.n_all;         // some row does not see all of the block
+            f32x4 sc[RT][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i) sc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f16x8 kk = operand(k[t][j][2 * h], k[t][j][2 * h + 1]);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) sc[i][t] = mma(kk, q[i][j][h][x], sc[i][t]);
+                    }
+            }
+            float k_mul[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) k_mul[c] = two_to((ks[c >> 2] >> (8 * (c & 3))) & 0xffu);
+            if (b + kKvqWaves < b1) load_k(b + kKvqWaves);
+            // entries behind the last position that is seen may be anything: their codes and scales are taken out
+            const int live = a.n - p0 - gq * 16;                       // of this lane's 16 positions
+            if (live < 16) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int l = live - 4 * w;
+                    const uint32_t keep = l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u;
+                    vs[w] &= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) v[d][w] &= keep;
+                }
+            }
+            int vb[16], top = 0;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+                vb[c] = (int)((vs[c >> 2] >> (8 * (c & 3))) & 0xffu);
+                top = vb[c] > top ? vb[c] : top;
+            }
+            f16x8 p[RT][2][2];                             // [.][k-step][hi, lo]
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                float w[16], bm = -INFINITY;
+                int e_new = top;
+                if (part_hidden) {                         // (what a row does not see has no part in its scale)
+                    e_new = 0;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const bool seen = p0 + gq * 16 + c <= see[i];
+                        w[c] = seen ? sc[i][c >> 2][c & 3] * q_mul[i] * k_mul[c] : -INFINITY;
+                        e_new = seen && vb[c] > e_new ? vb[c] : e_new;
+                        bm = fmaxf(bm, w[c]);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        w[c] = sc[i][c >> 2][c & 3] * q_mul[i] * k_mul[c];
+                        bm = fmaxf(bm, w[c]);
+                    }
+                }
+                bm = max_rows(bm);
+                e_new = (int)max_rows((float)e_new);
+                e_new = e_new > e_ref[i] ? e_new : e_ref[i];
+                const float shrink = ldexpf(1.0f, e_ref[i] - e_new);
+                e_ref[i] = e_new;
+                const float nm = fmaxf(mx[i], bm), ref = softmax_ref(nm), alpha = exp2_fast(mx[i] - ref);
+                mx[i] = nm;
+                float add = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    u16x8 hi8, lo8;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int c = h * 8 + e;
+                        const float x = exp2_fast(w[c] - ref);
+                        add += x;
+                        uint16_t hi, lo;
+                        split16<true>(ldexpf(x, vb[c] - e_new + kPBits), hi, lo);
+                        hi8[e] = hi;
+                        lo8[e] = lo;
+                    }
+                    p[i][h][0] = __builtin_bit_cast(f16x8, hi8);
+                    p[i][h][1] = __builtin_bit_cast(f16x8, lo8);
+                }
+                sum[i] = sum[i] * alpha + add;
+                const float f = alpha * shrink;
+                if (!__all(f == 1.0f)) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[i][d] *= f;
+                }
+            }
+            // a value that is not a number, at a position that only some rows see, must not reach the others by way of 0 * NaN
+            bool bad = false;
+            if (part_hidden) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t x = (v[d][w] & 0x7f7f7f7fu) + 0x01010101u;
+                        bad |= (x & 0x80808080u) != 0;
+                    }
+            }
+            if (part_hidden && __any(bad)) {
+                for (int t = 0; t < a.m; ++t) {
+                    const int l0 = a.see[t] + 1 - p0 - gq * 16;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t w[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int l = l0 - 4 * (2 * h + e);
+                                w[e] = v[d][2 * h + e] & (l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u);
+                            }
+                            const f16x8 vv = operand(w[0], w[1]);
+#pragma unroll
+                            for (int i = 0; i < RT; ++i) {
+                                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                                x = mma(vv, p[i][h][0], x);
+                                x = mma(vv, p[i][h][1], x);
+                                if (t_row[i] == t) o[i][d] += x;
+                            }
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f16x8 vv = operand(v[d][2 * h], v[d][2 * h + 1]);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) o[i][d] = mma(vv, p[i][h][x], o[i][d]);
+                    }
+            }
+            if (b + kKvqWaves < b1) load_v(b + kKvqWaves);
+        }
+        // lane (n, gq): row n of a tile, dimensions d * 16 + gq * 4 .. + 3.  The wavefronts' results are folded in wavefront order.
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int ni = nr - i * 16 < 16 ? nr - i * 16 : 16;        // rows of this tile
+            if (ni <= 0) break;
+            const float den = sum_rows(sum[i]), unit = ldexpf(1.0f, e_ref[i] - 127 - kPBits);
+            if (gq == 0) {
+                L.mx[wave][n] = mx[i];
+                L.sum[wave][n] = den;
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) *(f32x4 *)&L.part[wave][n][d * 16 + gq * 4] = o[i][d] * unit;
+            __syncthreads();
+            for (int idx = tid; idx < ni * (DH / 2); idx += 256) {
+                const int rr = idx / (DH / 2), d = idx % (DH / 2) * 2, r = r0 + i * 16 + rr;
+                float M = -INFINITY, sums = 0.f;
+                f32x2 num = {0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kKvqWaves; ++w) M = fmaxf(M, L.mx[w][rr]);
+                const float ref = softmax_ref(M);
+#pragma unroll
+                for (int w = 0; w < kKvqWaves; ++w) {
+                    const float f = exp2_fast(L.mx[w][rr] - ref);       // a wavefront without keys: exp(-inf) = 0, of sums that are 0
+                    const f32x2 x = *(const f32x2 *)&L.part[w][rr][d];
+                    sums += f * L.sum[w][rr];
+                    num[0] += f * x[0];
+                    num[1] += f * x[1];
+                }
+                if (a.S == 1) {
+                    kvq_output(a, g, r, d, num[0] / sums, num[1] / sums);
+                    continue;
+                }
+                float *out = a.part + (((size_t)g * a.S + s) * a.R + r) * PR;
+                *(f32x2 *)(out + d) = num;
+                if (d == 0) *(f32x2 *)(out + DH) = (f32x2){M, sums};
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Folds the items of a query row in their order: a workgroup per row, DH / 2 threads (two dimensions each) times groups that take every
+// NG-th item, a batch of them in flight.
+template <int DH>
+__global__ void __launch_bounds__(256) k_kvq_combine(KvqAttn a) {
+    constexpr int PR = DH + 2, TG = DH / 2, NG = 256 / TG, KB = 8;
+    __shared__ float st[NG][2];
+    __shared__ f32x2 part[NG][TG];
+    const int tid = threadIdx.x, grp = tid / TG, d = 2 * (tid % TG);
+    const int g = quotient((int)blockIdx.x, a.R, a.mul_R), r = (int)blockIdx.x - g * a.R;
+    const float *base = a.part + ((size_t)g * a.S * a.R + r) * PR;
+    float M = -INFINITY, den = 0.f;
+    f32x2 o = {0.f, 0.f};
+    for (int s0 = grp; s0 < a.S; s0 += NG * KB) {
+        f32x2 x[KB], ms[KB];
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {                          // items past the end repeat the group's first (weight 0)
+            const int s = s0 + i * NG < a.S ? s0 + i * NG : s0;
+            const float *p = base + (size_t)s * a.R * PR;
+            ms[i] = *(const f32x2 *)(p + DH);
+            x[i] = *(const f32x2 *)(p + d);
+        }
+        float nm = M;
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+            if (s0 + i * NG >= a.S) ms[i] = (f32x2){-INFINITY, 0.f};
+            nm = fmaxf(nm, ms[i][0]);
+        }
+        const float ref = softmax_ref(nm), alpha = exp2_fast(M - ref);
+        M = nm;
+        den *= alpha;
+        o *= alpha;
+#pragma unroll
+        for (int i = 0; i < KB; ++i) {
+            // (an item that this row sees nothing of has sums of 0 and a maximum of minus infinity)
+            const float w = exp2_fast(ms[i][0] - ref);
+            den += w * ms[i][1];
+            o[0] += w * x[i][0];
+            o[1] += w * x[i][1];
+        }
+    }
+    part[grp][tid % TG] = o;
+    if (d == 0) {
+        st[grp][0] = M;
+        st[grp][1] = den;
+    }
+    __syncthreads();
+    if (tid >= TG) return;
+    float m = -INFINITY, sum = 0.f;
+    f32x2 y = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NG; ++i) m = fmaxf(m, st[i][0]);
+    const float ref = softmax_ref(m);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+        const float w = exp2_fast(st[i][0] - ref);
+        sum += w * st[i][1];
+        y += w * part[i][tid];
+    }
+    kvq_output(a, g, r, d, y[0] / sum, y[1] / sum);
+}
+
+template <int DH>
+int launch_attn_dh(const KvqAttn &a, const LaunchCtx &c) {
+    const dim3 items(a.c.Hkv * a.S);
+    const int rc = a.R <= 16 ? launch<k_kvq_attn<DH, 1>>(c, items, dim3(256), 0, a) : launch<k_kvq_attn<DH, 2>>(c, items, dim3(256), 0, a);
+    if (rc || a.S == 1) return rc;
+    return launch<k_kvq_combine<DH>>(c, dim3(a.c.Hkv * a.R), dim3(256), 0, a);
+}
+
+bool rows_ok(const KvqRows &a) { return a.n >= 1 && a.pos0 >= 0 && (int64_t)a.pos0 + a.n <= a.c.stride && a.ld % 4 == 0; }
+dim3 rows_grid(const KvqRows &a) { return dim3((a.pos0 + a.n - 1) / kKvqBlock - a.pos0 / kKvqBlock + 1, a.c.Hkv); }
+
+}  // namespace
+
+int launch_kvq_store(const KvqRows &a, const LaunchCtx &c) {
+    if (!rows_ok(a)) return (int)hipErrorInvalidValue;
+    if (a.c.dh == 128) return launch<k_kvq_store<128>>(c, rows_grid(a), dim3(256), 0, a);
+    if (a.c.dh == 64) return launch<k_kvq_store<64>>(c, rows_grid(a), dim3(256), 0, a);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_kvq_read(const KvqRows &a, const LaunchCtx &c) {
+    if (!rows_ok(a)) return (int)hipErrorInvalidValue;
+    if (a.c.dh == 128) return launch<k_kvq_read<128>>(c, rows_grid(a), dim3(256), 0, a);
+    if (a.c.dh == 64) return launch<k_kvq_read<64>>(c, rows_grid(a), dim3(256), 0, a);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_kvq_rotate(const KvqRotate &a, const LaunchCtx &c) {
+    if (a.m < 1 || a.pos0 < 0 || (int64_t)a.pos0 + a.m > a.c.stride) return (int)hipErrorInvalidValue;
+    const dim3 grid((a.m * (a.Hq + 2 * a.c.Hkv) + 3) / 4);
+    if (a.c.dh == 128) return launch<k_kvq_rotate<128>>(c, grid, dim3(256), 0, a);
+    if (a.c.dh == 64) return launch<k_kvq_rotate<64>>(c, grid, dim3(256), 0, a);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_kvq_expand(const KvqExpand &a, const LaunchCtx &c) {
+    if (a.n < 1 || a.n > a.c.stride) return (int)hipErrorInvalidValue;
+    const dim3 grid((a.n + kKvqBlock - 1) / kKvqBlock, a.c.Hkv);
+    if (a.c.dh == 128) return launch<k_kvq_expand<128>>(c, grid, dim3(256), 0, a);
+    if (a.c.dh == 64) return launch<k_kvq_expand<64>>(c, grid, dim3(256), 0, a);
+    return (int)hipErrorInvalidValue;
+}
+
+// Items: one per compute unit, but no fewer blocks than an item has wavefronts; contexts of up to two blocks per wavefront are one item
+// per kv head, which writes the output itself.
+void kvq_attn_finish(KvqAttn &a, int n_wg) {
+    a.G = a.Hq / a.c.Hkv;
+    a.R = a.G * a.m;
+    a.n = a.n_all = a.see[0] + 1;
+    for (int t = 1; t < a.m; ++t) {
+        a.n = a.see[t] + 1 > a.n ? a.see[t] + 1 : a.n;
+        a.n_all = a.see[t] + 1 < a.n_all ? a.see[t] + 1 : a.n_all;
+    }
+    const int blocks = (a.n + kKvqBlock - 1) / kKvqBlock;
+    int S = n_wg / a.c.Hkv;
+    if (S > blocks / kKvqWaves) S = blocks / kKvqWaves;
+    if (S > kKvqMaxSplits) S = kKvqMaxSplits;
+    if (S < 1 || blocks <= 2 * kKvqWaves) S = 1;
+    a.per = (blocks + S - 1) / S;
+    a.S = (blocks + a.per - 1) / a.per;
+    a.mul_S = div_multiplier(a.S);
+    a.mul_G = div_multiplier(a.G);
+    a.mul_R = div_multiplier(a.R);
+}
+
+int launch_kvq_attn(const KvqAttn &a, const LaunchCtx &c) {
+    if (a.m < 1 || a.m > 8 || a.n < 1 || a.n > a.c.stride || a.S < 1 || a.S > kvq_max_splits(a.c.stride) || (int64_t)a.S * a.per * kKvqBlock < a.n) return (int)hipErrorInvalidValue;
+    if (a.c.dh == 128) return launch_attn_dh<128>(a, c);
+    if (a.c.dh == 64) return launch_attn_dh<64>(a, c);
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace ad

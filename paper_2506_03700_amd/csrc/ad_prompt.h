@@ -65,13 +65,15 @@ struct PromptQkv {
     void *Q;                  // per kv head, query rows r = t * G + head in group: tiles of 16 rows, [tile][ks][plane][lane][8]
     float q_scale;            // 1 / sqrt(dh)
     int f16;
+    float *k_rows, *v_rows;   // 8-bit cache: rotated keys and values go here instead, fp32 [M][Hkv * dh] (else null)
 };
 
 struct PromptAttn {
     const void *Q, *Kc, *Vc;
     int stride, pos0, M, Hq, Hkv, dh, G, q_rows;
     void *Bo;                 // activation tiles of the Wo projection
-    int Bo_KT, f16;
+    int Bo_KT, f16;           // f16: queries, keys and values are fp16 (else bf16)
+    int f16_out;              // the tiles of Bo are
 };
 
 constexpr int kPromptEmbedRows = 512;      // token ids travel in the kernel arguments

@@ -398,7 +398,8 @@ constexpr int kQkvAlign = 64;           // V's dead positions are cleared up to 
 constexpr int kFewTokens = 256;         // up to here workgroups of 16 tokens, and above of twice the threads per token: larger ones would leave
                                         // compute units idle (63 tokens of the 8B shape: 48 workgroups of 64, 10.6 us, now 192)
 
-template <int DH, int kQkvTokens, bool F16>
+// ROWS: keys and values leave as fp32 rows, which the 8-bit cache's store takes
+template <int DH, int kQkvTokens, bool F16, bool ROWS>
 __global__ void __launch_bounds__(256) k_prompt_qkv(PromptQkv a) {
     constexpr int half = DH / 2, NC = half / 8;         // groups of 8 dimensions in the lower half
     const int t0 = blockIdx.x * kQkvTokens, head = a.head0 + blockIdx.y, tid = threadIdx.x;
@@ -454,6 +455,13 @@ __global__ void __launch_bounds__(256) k_prompt_qkv(PromptQkv a) {
                 Q[act_unit(r, c * 8, DH / 32, 1)] = l0;
                 Q[act_unit(r, half + c * 8, DH / 32, 0)] = h1;
                 Q[act_unit(r, half + c * 8, DH / 32, 1)] = l1;
+            } else if constexpr (ROWS) {
+                float *K = a.k_rows + ((size_t)t * a.Hkv + (head - a.Hq)) * DH;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    *(f32x4 *)(K + c * 8 + 4 * h) = (f32x4){r0[4 * h], r0[4 * h + 1], r0[4 * h + 2], r0[4 * h + 3]};
+                    *(f32x4 *)(K + half + c * 8 + 4 * h) = (f32x4){r1[4 * h], r1[4 * h + 1], r1[4 * h + 2], r1[4 * h + 3]};
+                }
             } else {
                 uint16_t *K = (uint16_t *)a.Kc + ((size_t)(head - a.Hq) * a.stride + a.pos0 + t) * DH;
                 u16x8 k0, k1;
@@ -465,6 +473,16 @@ __global__ void __launch_bounds__(256) k_prompt_qkv(PromptQkv a) {
                 *(u16x8 *)(K + c * 8) = k0;
                 *(u16x8 *)(K + half + c * 8) = k1;
             }
+        }
+    } else if constexpr (ROWS) {
+        for (int idx = tid; idx < kQkvTokens * (DH / 8); idx += 256) {
+            const int tl = idx / (DH / 8), c = idx % (DH / 8), t = t0 + tl;
+            if (t >= a.M) break;
+            float x[8];
+            load8(t, c * 8, x);
+            float *V = a.v_rows + ((size_t)t * a.Hkv + (head - a.Hq - a.Hkv)) * DH + c * 8;
+            *(f32x4 *)V = (f32x4){x[0], x[1], x[2], x[3]};
+            *(f32x4 *)(V + 4) = (f32x4){x[4], x[5], x[6], x[7]};
         }
     } else {
         // V is kept transposed: through LDS, then 8 positions of a dimension per store.  Positions past the prompt, up to the
@@ -499,7 +517,7 @@ __global__ void __launch_bounds__(256) k_prompt_qkv(PromptQkv a) {
 // side, beat 32: 8B shape, 299 / 511 / 1023 tokens 15.3 / 23.2 / 48.2 -> 14.3 / 20.1 / 40.6 us, 13B 16.5 (299) / 47.3 (1023) -> 14.4 / 41.6.
 constexpr int kPromptAttnRows = 64;
 
-template <int DH, bool F16>
+template <int DH, bool F16, bool F16_OUT>
 __global__ void __launch_bounds__(256, 2) k_prompt_attn(PromptAttn a) {
     constexpr int KS = DH / 32, DT = DH / 16;
     constexpr int KU = 2 * KS * 64, VU = DT * 64, HU = KU + VU;  // 16-byte units of 32 positions: K tiles, V tiles, both
@@ -624,7 +642,7 @@ __global__ void __launch_bounds__(256, 2) k_prompt_attn(PromptAttn a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 uint16_t hi, lo;
-                split16<F16>(o[d][e] * inv, hi, lo);
+                split16<F16_OUT>(o[d][e] * inv, hi, lo);
                 h4[e] = hi;
                 l4[e] = lo;
             }
@@ -705,31 +723,38 @@ int launch_prompt_rows(const PromptRows &a, void *stream) {
     return (int)hipGetLastError();
 }
 
-template <int DH, bool F16>
+template <int DH, bool F16, bool ROWS>
 static int launch_qkv_as(const PromptQkv &a, hipStream_t s) {
     const int n = (a.M + kQkvAlign - 1) / kQkvAlign * kQkvAlign, heads = a.Hq + 2 * a.Hkv - a.head0;
-    if (a.M <= kFewTokens) hipLaunchKernelGGL((k_prompt_qkv<DH, 16, F16>), dim3(n / 16, heads), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_prompt_qkv<DH, 64, F16>), dim3(n / 64, heads), dim3(256), 0, s, a);
+    if (a.M <= kFewTokens) hipLaunchKernelGGL((k_prompt_qkv<DH, 16, F16, ROWS>), dim3(n / 16, heads), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_prompt_qkv<DH, 64, F16, ROWS>), dim3(n / 64, heads), dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 int launch_prompt_qkv(const PromptQkv &a, void *stream) {
     hipStream_t s = (hipStream_t)stream;
     if (a.pos0 % kQkvAlign) return (int)hipErrorInvalidValue;
-    if (a.dh == 128) return a.f16 ? launch_qkv_as<128, true>(a, s) : launch_qkv_as<128, false>(a, s);
-    if (a.dh == 64) return a.f16 ? launch_qkv_as<64, true>(a, s) : launch_qkv_as<64, false>(a, s);
+    if (a.k_rows) {                  // (the queries meet an 8-bit cache's values in bf16, whatever the model's type)
+        if (a.f16) return (int)hipErrorInvalidValue;
+        if (a.dh == 128) return launch_qkv_as<128, false, true>(a, s);
+        if (a.dh == 64) return launch_qkv_as<64, false, true>(a, s);
+        return (int)hipErrorInvalidValue;
+    }
+    if (a.dh == 128) return a.f16 ? launch_qkv_as<128, true, false>(a, s) : launch_qkv_as<128, false, false>(a, s);
+    if (a.dh == 64) return a.f16 ? launch_qkv_as<64, true, false>(a, s) : launch_qkv_as<64, false, false>(a, s);
     return (int)hipErrorInvalidValue;
 }
 
-template <int DH, bool F16>
+template <int DH, bool F16, bool F16_OUT>
 static int launch_attn_as(const PromptAttn &a, hipStream_t s) {
     const int n_blk = (a.M * a.G + kPromptAttnRows - 1) / kPromptAttnRows;
-    hipLaunchKernelGGL((k_prompt_attn<DH, F16>), dim3(n_blk * a.Hkv), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prompt_attn<DH, F16, F16_OUT>), dim3(n_blk * a.Hkv), dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 int launch_prompt_attn(const PromptAttn &a, void *stream) {
     hipStream_t s = (hipStream_t)stream;
-    if (a.dh == 128) return a.f16 ? launch_attn_as<128, true>(a, s) : launch_attn_as<128, false>(a, s);
-    if (a.dh == 64) return a.f16 ? launch_attn_as<64, true>(a, s) : launch_attn_as<64, false>(a, s);
+    if (a.f16 && !a.f16_out) return (int)hipErrorInvalidValue;
+    if (a.dh == 128) return a.f16 ? launch_attn_as<128, true, true>(a, s) : a.f16_out ? launch_attn_as<128, false, true>(a, s) : launch_attn_as<128, false, false>(a, s);
+    if (a.dh == 64) return a.f16 ? launch_attn_as<64, true, true>(a, s) : a.f16_out ? launch_attn_as<64, false, true>(a, s) : launch_attn_as<64, false, false>(a, s);
     return (int)hipErrorInvalidValue;
 }
 
