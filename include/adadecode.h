@@ -238,6 +238,36 @@ ad_status ad_verify_sampled_wait(const ad_model *, const void *final_logits, con
                                  int32_t m, float temperature, const float *u_accept, const float *u_resample, float u_final,
                                  int32_t *n_accept, int32_t *next_token, float *ratio, void *stream);
 
+/* ---- filtered distributions: what top-k, top-p and min-p leave of softmax(z / temperature) for sampled decoding.
+ * The ids of a row are ordered by logit, largest first, equal ones by id.  Kept are the first top_k of them; of those, the ids before
+ * which less than top_p of the weight of those top_k lies; and of those, the ids whose probability is at least min_p times the largest.  At least one
+ * id is kept, an id whose logit is minus infinity never; the kept probabilities are scaled to a sum of 1.  Borders and sums are
+ * those of 64-bit arithmetic (ids of less than 2^-61 * vocab of the largest one's probability have no share in a sum or draw), and do not depend on the order of anything: the same call
+ * gives the same bits.  A row with a logit that is no number or plus infinity, or without one above minus infinity, has no distribution: its
+ * probabilities are no numbers, a draw from it is token -1 with a probability that is no number. */
+typedef struct {
+    float   temperature;         /* > 0, finite */
+    int32_t top_k;               /* 0: off */
+    float   top_p;               /* in [0, 1]; 0 and 1: off */
+    float   min_p;               /* in [0, 1]; 0: off */
+} ad_filter;
+
+/* probs[r] = the filtered distribution of logits[r], 0 for ids that are not kept.  logits, probs: dev [m, vocab] fp32, apart from each
+ * other; m in 1..m_max. */
+ad_status ad_filtered_probs(const ad_model *, const void *logits, int32_t m, const ad_filter *, void *probs, void *stream);
+/* ad_sample_logits and ad_verify_sampled between filtered distributions, the final rows' and the drafts' through the same filter.  A draft that its own
+ * distribution does not hold has the ratio infinity (accepted) or, if the final one does not hold it either, 0.  All three, and the calls that wait, use
+ * the model's scratch: calls on one model must be stream-ordered. */
+ad_status ad_sample_filtered(const ad_model *, const void *logits, const ad_filter *, float u, int32_t *token, float *prob, void *stream);
+ad_status ad_verify_filtered(const ad_model *, const void *final_logits, const void *draft_logits, const int32_t *draft, int32_t m,
+                             const ad_filter *, const float *u_accept, const float *u_resample, float u_final, int32_t *n_accept,
+                             int32_t *next_token, float *ratio, void *stream);
+/* The same, returning with their results as ad_sample_logits_wait and ad_verify_sampled_wait do. */
+ad_status ad_sample_filtered_wait(const ad_model *, const void *logits, const ad_filter *, float u, int32_t *token, float *prob, void *stream);
+ad_status ad_verify_filtered_wait(const ad_model *, const void *final_logits, const void *draft_logits, const int32_t *draft, int32_t m,
+                                  const ad_filter *, const float *u_accept, const float *u_resample, float u_final, int32_t *n_accept,
+                                  int32_t *next_token, float *ratio, void *stream);
+
 /* ---- Algorithm 1 --------------------------------------------------------------------------------- */
 typedef struct {
     float   gamma;               /* early-prediction threshold of Eq. 1 (strict >) */
@@ -294,6 +324,13 @@ typedef struct { int32_t kind, layer, pos, m, token, flag; float conf; float res
 ad_status ad_generate(const ad_model *, ad_kv *, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *,
                       int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
                       int64_t *n_events, void *stream);
+
+/* ad_generate in sampled decoding with a filter on every draw and on both sides of every verification; the probability compared with gamma is the
+ * filtered distribution's.  The filter's temperature stands in for that of the parameters, whose uniforms are needed.  A filter whose steps are
+ * all off is ad_generate at that temperature. */
+ad_status ad_generate_filtered(const ad_model *, ad_kv *, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *, const ad_filter *,
+                               int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
+                               int64_t *n_events, void *stream);
 
 /* ---- measurement ------------------------------------------------------------------------------------
  * Samples one of the library's two big kernels: AD_PROF_GEMM, the weight-streaming GEMM kernel (the vocabulary

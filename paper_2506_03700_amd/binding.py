@@ -29,7 +29,8 @@ EXPORTS = ["ad_workspace_bytes", "ad_model_create", "ad_model_destroy", "ad_kv_b
            "ad_verify_static", "ad_exit_head_wait", "ad_verify_wait", "ad_sample_logits_wait", "ad_verify_sampled_wait",
            "ad_head_logits", "ad_sample_logits", "ad_verify_sampled", "ad_generate", "ad_layer_trace", "ad_profile_start", "ad_profile_stop", "ad_probe_stream",
            "ad_last_error", "ad_version",
-           "ad_kvq_bytes", "ad_kvq_create", "ad_kvq_append", "ad_kvq_read", "ad_kvq_attend"]
+           "ad_kvq_bytes", "ad_kvq_create", "ad_kvq_append", "ad_kvq_read", "ad_kvq_attend",
+           "ad_filtered_probs", "ad_sample_filtered", "ad_verify_filtered", "ad_sample_filtered_wait", "ad_verify_filtered_wait", "ad_generate_filtered"]
 
 
 class Config(C.Structure):
@@ -51,6 +52,11 @@ class GenParams(C.Structure):
     _fields_ = [("gamma", C.c_float), ("max_pending", C.c_int32), ("max_new", C.c_int32), ("eos_id", C.c_int32),
                 ("forced_exit", C.c_void_p), ("scripted_draft", C.c_void_p), ("temperature", C.c_float), ("uniforms", C.c_void_p),
                 ("head_mask", C.c_int32), ("no_verify", C.c_int32), ("no_issue_ahead", C.c_int32)]
+
+
+class Filter(C.Structure):
+    """ad_filter: Filter(temperature, top_k, top_p, min_p); 0 leaves a step out."""
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 class Stats(C.Structure):
@@ -112,9 +118,13 @@ def lib() -> C.CDLL:
         L.ad_head_logits.argtypes = [P, i32, P, i32, P, P]
         L.ad_sample_logits.argtypes = [P, P, C.c_float, C.c_float, P, P, P]
         L.ad_verify_sampled.argtypes = [P, P, P, P, i32, C.c_float, P, P, C.c_float, P, P, P, P]
-        for n in ("exit_head", "verify", "sample_logits", "verify_sampled"):
+        L.ad_filtered_probs.argtypes = [P, P, i32, C.POINTER(Filter), P, P]
+        L.ad_sample_filtered.argtypes = [P, P, C.POINTER(Filter), C.c_float, P, P, P]
+        L.ad_verify_filtered.argtypes = [P, P, P, P, i32, C.POINTER(Filter), P, P, C.c_float, P, P, P, P]
+        for n in ("exit_head", "verify", "sample_logits", "verify_sampled", "sample_filtered", "verify_filtered"):
             getattr(L, f"ad_{n}_wait").argtypes = getattr(L, "ad_" + n).argtypes
         L.ad_generate.argtypes = [P, P, P, i32, C.POINTER(GenParams), P, P, C.POINTER(Stats), P, C.c_int64, P, P]
+        L.ad_generate_filtered.argtypes = L.ad_generate.argtypes[:5] + [C.POINTER(Filter)] + L.ad_generate.argtypes[5:]
         L.ad_profile_start.argtypes = [P, i32, i32, i32]
         L.ad_set_layer_mode.argtypes = [P, i32]
         L.ad_layer_trace.argtypes = [P, P, C.c_size_t, P, P]
@@ -429,14 +439,48 @@ class Model:
         res = out.numpy()
         return int(res[8]), int(res[9]), res[16:16 + m - 1].view(np.float32).copy()
 
+    def ad_filtered_probs(self, logits, flt: Filter):
+        """The filtered distributions of rows of logits, float32 [m, vocab]."""
+        torch = self.torch
+        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.dim() == 2 and logits.shape[1] == self.shape.vocab
+        p = torch.empty_like(logits)
+        _check(self.L.ad_filtered_probs(self.model, logits.data_ptr(), logits.shape[0], C.byref(flt), p.data_ptr(), _stream_ptr(torch)))
+        return p
+
+    def ad_sample_filtered(self, logits, flt: Filter, u: float):
+        """(token, its probability) drawn from the filtered distribution with the uniform draw u."""
+        torch = self.torch
+        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.numel() == self.shape.vocab
+        tok, prob = C.c_int32(), C.c_float()
+        _check(self.L.ad_sample_filtered_wait(self.model, logits.data_ptr(), C.byref(flt), u, C.byref(tok), C.byref(prob), _stream_ptr(torch)))
+        return tok.value, prob.value
+
+    def ad_verify_filtered(self, final_logits, draft_logits, draft: Sequence[int], flt: Filter, u_accept, u_resample, u_final: float):
+        """Eq. 2 between filtered distributions: (n_accept, next_token, ratios[m-1])."""
+        torch = self.torch
+        m, V = final_logits.shape
+        assert final_logits.dtype == torch.float32 and final_logits.is_contiguous() and V == self.shape.vocab
+        d = np.ascontiguousarray(draft, dtype=np.int32)
+        ua = np.ascontiguousarray(u_accept, dtype=np.float32)
+        ur = np.ascontiguousarray(u_resample, dtype=np.float32)
+        assert d.size == ua.size == ur.size == m - 1
+        if m > 1:
+            assert draft_logits.dtype == torch.float32 and draft_logits.is_contiguous() and tuple(draft_logits.shape) == (m - 1, V)
+        n, nxt, ratio = C.c_int32(), C.c_int32(), np.empty(m - 1, dtype=np.float32)
+        at = lambda a: a.ctypes.data if m > 1 else None
+        _check(self.L.ad_verify_filtered_wait(self.model, final_logits.data_ptr(), draft_logits.data_ptr() if m > 1 else None, at(d), m, C.byref(flt),
+                                              at(ua), at(ur), u_final, C.byref(n), C.byref(nxt), at(ratio), _stream_ptr(torch)))
+        return n.value, nxt.value, ratio
+
     def ad_generate(self, prompt, max_new: int, gamma: float, max_pending: int = 5, eos_id: int = -1,
                     forced_exit: Optional[np.ndarray] = None, scripted_draft: Optional[np.ndarray] = None,
                     max_events: int = 1 << 20, want_events: bool = True, temperature: float = 0.0,
                     uniforms: Optional[np.ndarray] = None, head_mask: int = 0, no_verify: bool = False,
-                    no_issue_ahead: bool = False):
+                    no_issue_ahead: bool = False, top_k: int = 0, top_p: float = 0.0, min_p: float = 0.0):
         """temperature > 0: sampled decoding with the draws `uniforms`, float32 [max_pos, n_exit + 3].
         head_mask / no_verify: ablation switches (bit i enables exit head i; drafts are kept unchecked).
-        no_issue_ahead: nothing is issued behind a head evaluation before its outcome is known."""
+        no_issue_ahead: nothing is issued behind a head evaluation before its outcome is known.
+        top_k, top_p, min_p: filters of sampled decoding (0: off)."""
         torch = self.torch
         p = np.ascontiguousarray(prompt, dtype=np.int32)
         if temperature > 0:
@@ -456,9 +500,11 @@ class Model:
         out = np.empty(max_new, dtype=np.int32)
         ev = np.zeros(max_events if want_events else 1, dtype=EVENT_DTYPE)
         n, nev, st = C.c_int32(), C.c_int64(), Stats()
-        _check(self.L.ad_generate(self.model, self.kv, p.ctypes.data, p.size, C.byref(gp), out.ctypes.data, C.byref(n), C.byref(st),
-                                  ev.ctypes.data if want_events else None, max_events if want_events else 0, C.byref(nev),
-                                  _stream_ptr(torch)))
+        generate, more = self.L.ad_generate, ()
+        if top_k or top_p or min_p:
+            generate, more = self.L.ad_generate_filtered, (C.byref(Filter(temperature, top_k, top_p, min_p)),)
+        _check(generate(self.model, self.kv, p.ctypes.data, p.size, C.byref(gp), *more, out.ctypes.data, C.byref(n), C.byref(st),
+                        ev.ctypes.data if want_events else None, max_events if want_events else 0, C.byref(nev), _stream_ptr(torch)))
         return out[:n.value].copy(), st.as_dict(), ev[:min(nev.value, len(ev))].copy() if want_events else None
 
 

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/adadecode.h"
+#include "ad_filter.h"
 #include "ad_internal.h"
 #include "ad_kvq.h"
 #include "ad_prompt.h"
@@ -130,6 +131,7 @@ void make_layout(const ad_config &c, Layout &L) {
     s += align_up((size_t)kBarrierWords * 4);                  // grid-barrier counters of the fused layer step
     s += align_up((size_t)kArrivalWords * 4);                  // the sampling kernels' counter of workgroups
     s += 2 * align_up((size_t)AD_M_MAX * L.V * 4);             // sampled decoding: draft and final logits of the open rows
+    s += align_up(sizeof(FilterScratch));
     L.scratch_bytes = s;
     L.total = off + s;
 }
@@ -158,6 +160,7 @@ struct ad_model {
     float *ssq, *ssq_q;
     float *qkv, *x1, *rows, *head_part;
     float *draft_logits, *final_logits;   // sampled decoding
+    FilterScratch *filter;
     // pinned host results of the calls that wait for them
     int32_t *pin;         // [0..8) tok, [8] n_accept, [9] next, [16..24) row argmax, [28] the done word
     mutable int32_t done_seq = 0;   // last value asked for in the done word (unique per evaluation of this model)
@@ -289,6 +292,7 @@ ad_status ad_model_create(const ad_config *cfg, const ad_layer_weights *layers, 
     m->arrivals = (unsigned *)take((size_t)kArrivalWords * 4);    // likewise
     m->draft_logits = (float *)take((size_t)AD_M_MAX * L.V * 4);
     m->final_logits = (float *)take((size_t)AD_M_MAX * L.V * 4);
+    m->filter = (FilterScratch *)take(sizeof(FilterScratch));     // zeroed likewise
     m->pin = (int32_t *)pinned_alloc(4096);
     if (!m->pin) { delete m; return (ad_status)fail(AD_ENOMEM, "ad_model_create: pinned allocation failed"); }
     memset(m->pin, 0, 4096);      // recycled memory may hold an earlier model's done word, which would end the first wait at once
@@ -1005,6 +1009,77 @@ ad_status ad_verify_sampled(const ad_model *m, const void *final_logits, const v
                                      ratio, stream, nullptr, 0);
 }
 
+// ---- filtered distributions ----------------------------------------------------------------------------
+static int filter_args(const ad_model *m, const ad_filter *f, FilterArgs &a, const char *who) {
+    if (!(f->temperature > 0.f) || !(f->temperature < INFINITY)) return fail(AD_ERANGE, "%s: temperature must be > 0 and finite", who);
+    if (f->top_k < 0) return fail(AD_ERANGE, "%s: top_k must not be negative", who);
+    if (!(f->top_p >= 0.f && f->top_p <= 1.f) || !(f->min_p >= 0.f && f->min_p <= 1.f)) return fail(AD_ERANGE, "%s: top_p and min_p must be in [0, 1]", who);
+    memset(&a, 0, sizeof a);
+    a.V = m->cfg.vocab;
+    a.s = m->filter;
+    filter_finish(a, f->temperature, f->top_k, f->top_p, f->min_p);
+    return AD_OK;
+}
+
+ad_status ad_filtered_probs(const ad_model *m, const void *logits, int32_t n, const ad_filter *f, void *probs, void *stream) {
+    if (!m || !logits || !f || !probs) return (ad_status)fail(AD_EINVAL, "ad_filtered_probs: null argument");
+    if (n < 1 || n > m->cfg.m_max) return (ad_status)fail(AD_ERANGE, "ad_filtered_probs: m = %d outside 1..%d", n, m->cfg.m_max);
+    FilterArgs a;
+    int rc = filter_args(m, f, a, "ad_filtered_probs");
+    if (rc) return (ad_status)rc;
+    a.z0 = (const float *)logits; a.n_first = a.rows = n;
+    rc = launch_filter_probs(a, (float *)probs, launch_ctx(m, stream));
+    return rc ? (ad_status)hip_fail(rc, "ad_filtered_probs") : AD_OK;
+}
+
+static int sample_filtered(const ad_model *m, const void *logits, const ad_filter *f, float u, int32_t *token, float *prob, void *stream,
+                           int32_t *done_flag, int32_t done_seq) {
+    if (!m || !logits || !f || !token || !prob) return fail(AD_EINVAL, "ad_sample_filtered: null argument");
+    if (!(u >= 0.f && u < 1.f)) return fail(AD_ERANGE, "ad_sample_filtered: u must be in [0, 1)");
+    FilterArgs a;
+    int rc = filter_args(m, f, a, "ad_sample_filtered");
+    if (rc) return rc;
+    a.z0 = (const float *)logits; a.n_first = a.rows = 1; a.u = u; a.tok_out = token; a.prob_out = prob;
+    a.done_flag = done_flag; a.done_seq = done_seq;
+    rc = launch_filter_sample(a, launch_ctx(m, stream));
+    return rc ? hip_fail(rc, "ad_sample_filtered") : AD_OK;
+}
+
+ad_status ad_sample_filtered(const ad_model *m, const void *logits, const ad_filter *f, float u, int32_t *token, float *prob, void *stream) {
+    return (ad_status)sample_filtered(m, logits, f, u, token, prob, stream, nullptr, 0);
+}
+
+static int verify_filtered(const ad_model *m, const void *final_logits, const void *draft_logits, const int32_t *draft, int32_t n, const ad_filter *f,
+                           const float *u_accept, const float *u_resample, float u_final, int32_t *n_accept, int32_t *next_token, float *ratio,
+                           void *stream, int32_t *done_flag, int32_t done_seq) {
+    if (!m || !final_logits || !f || !n_accept || !next_token || (n > 1 && (!draft || !draft_logits || !u_accept || !u_resample)))
+        return fail(AD_EINVAL, "ad_verify_filtered: null argument");
+    if (n < 1 || n > m->cfg.m_max) return fail(AD_ERANGE, "ad_verify_filtered: m = %d outside 1..%d", n, m->cfg.m_max);
+    if (!(u_final >= 0.f && u_final < 1.f)) return fail(AD_ERANGE, "ad_verify_filtered: draws must be in [0, 1)");
+    FilterVerifyArgs v;
+    memset(&v, 0, sizeof v);
+    int rc = filter_args(m, f, v.f, "ad_verify_filtered");
+    if (rc) return rc;
+    for (int i = 0; i + 1 < n; ++i) {
+        if (draft[i] < 0 || draft[i] >= m->cfg.vocab) return fail(AD_ERANGE, "ad_verify_filtered: draft token outside the vocabulary");
+        if (!(u_accept[i] >= 0.f && u_accept[i] < 1.f) || !(u_resample[i] >= 0.f && u_resample[i] < 1.f))
+            return fail(AD_ERANGE, "ad_verify_filtered: draws must be in [0, 1)");
+        v.draft[i] = draft[i]; v.u_accept[i] = u_accept[i]; v.u_resample[i] = u_resample[i];
+    }
+    v.f.z0 = (const float *)final_logits; v.f.z1 = (const float *)draft_logits; v.f.n_first = n; v.f.rows = 2 * n - 1;
+    v.f.done_flag = done_flag; v.f.done_seq = done_seq;
+    v.m = n; v.u_final = u_final; v.n_accept_out = n_accept; v.next_out = next_token; v.ratio_out = ratio;
+    rc = launch_filter_verify(v, launch_ctx(m, stream));
+    return rc ? hip_fail(rc, "ad_verify_filtered") : AD_OK;
+}
+
+ad_status ad_verify_filtered(const ad_model *m, const void *final_logits, const void *draft_logits, const int32_t *draft, int32_t n,
+                             const ad_filter *f, const float *u_accept, const float *u_resample, float u_final, int32_t *n_accept,
+                             int32_t *next_token, float *ratio, void *stream) {
+    return (ad_status)verify_filtered(m, final_logits, draft_logits, draft, n, f, u_accept, u_resample, u_final, n_accept, next_token, ratio, stream,
+                                      nullptr, 0);
+}
+
 // ---- the same with the wait for the results ------------------------------------------------------------
 // The GPU idles from an evaluation's last kernel until the host's next launch arrives, and waiting for the stream to drain adds
 // the runtime's completion path to that gap; instead the last kernel publishes a sequence number in pinned memory after its
@@ -1073,6 +1148,28 @@ ad_status ad_verify_sampled_wait(const ad_model *m, const void *final_logits, co
     int rc = verify_sampled(m, final_logits, draft_logits, draft, n, temperature, u_accept, u_resample, u_final, m->pin + 8, m->pin + 9,
                             m->pin_conf + 8, stream, done_flag(m), next_seq(m));
     if (rc || (rc = wait_done(m, stream, "ad_verify_sampled_wait"))) return (ad_status)rc;
+    *n_accept = m->pin[8];
+    *next_token = m->pin[9];
+    if (ratio) memcpy(ratio, m->pin_conf + 8, sizeof(float) * (size_t)(n - 1));
+    return AD_OK;
+}
+
+ad_status ad_sample_filtered_wait(const ad_model *m, const void *logits, const ad_filter *f, float u, int32_t *token, float *prob, void *stream) {
+    if (!m || !token || !prob) return (ad_status)fail(AD_EINVAL, "ad_sample_filtered_wait: null argument");
+    int rc = sample_filtered(m, logits, f, u, m->pin, m->pin_conf, stream, done_flag(m), next_seq(m));
+    if (rc || (rc = wait_done(m, stream, "ad_sample_filtered_wait"))) return (ad_status)rc;
+    *token = m->pin[0];
+    *prob = m->pin_conf[0];
+    return AD_OK;
+}
+
+ad_status ad_verify_filtered_wait(const ad_model *m, const void *final_logits, const void *draft_logits, const int32_t *draft, int32_t n,
+                                  const ad_filter *f, const float *u_accept, const float *u_resample, float u_final, int32_t *n_accept,
+                                  int32_t *next_token, float *ratio, void *stream) {
+    if (!m || !n_accept || !next_token) return (ad_status)fail(AD_EINVAL, "ad_verify_filtered_wait: null argument");
+    int rc = verify_filtered(m, final_logits, draft_logits, draft, n, f, u_accept, u_resample, u_final, m->pin + 8, m->pin + 9, m->pin_conf + 8, stream,
+                             done_flag(m), next_seq(m));
+    if (rc || (rc = wait_done(m, stream, "ad_verify_filtered_wait"))) return (ad_status)rc;
     *n_accept = m->pin[8];
     *next_token = m->pin[9];
     if (ratio) memcpy(ratio, m->pin_conf + 8, sizeof(float) * (size_t)(n - 1));
@@ -1176,6 +1273,7 @@ struct GpuBackend : Backend {
     ad_kv *kv;
     void *stream;
     int64_t bytes = 0;
+    ad_filter filter{0.f, 0, 0.f, 0.f};   // sampled decoding; its temperature is the scheduler's to say
     bool in_prefill = false;   // the prompt pass is not part of the decode-step byte count
     int32_t pos_buf[AD_M_MAX];
 
@@ -1264,12 +1362,17 @@ struct GpuBackend : Backend {
         bytes += (int64_t)m->cfg.vocab * m->cfg.d_model * s;
         return AD_OK;
     }
+    const ad_filter *filter_at(float temperature) {      // null: a temperature alone
+        filter.temperature = temperature;
+        return filter.top_k || (filter.top_p > 0.f && filter.top_p < 1.f) || filter.min_p > 0.f ? &filter : nullptr;
+    }
     // Eq. 1 with a sampled token: the head's logits stay in the draft slot of this row until the verification
     int sample_head(int32_t layer, int32_t r, int32_t, float temperature, float u, int32_t *token, float *prob) override {
         float *z = m->draft_logits + (size_t)r * m->cfg.vocab;
         hint.kind = issued.kind = AHEAD_NONE;
         int rc = ad_head_logits(m, layer, row(r), 1, z, stream);
-        if (rc == AD_OK) rc = ad_sample_logits_wait(m, z, temperature, u, token, prob, stream);
+        const ad_filter *f = filter_at(temperature);
+        if (rc == AD_OK) rc = f ? ad_sample_filtered_wait(m, z, f, u, token, prob, stream) : ad_sample_logits_wait(m, z, temperature, u, token, prob, stream);
         if (rc != AD_OK) return rc;
         if ((rc = fused_health(m, stream))) return rc;
         const int64_t s = m->cfg.dtype == AD_F32 ? 4 : 2;
@@ -1280,9 +1383,11 @@ struct GpuBackend : Backend {
                        float u_final, int32_t *n_accept, int32_t *next, float *ratio) override {
         hint.kind = issued.kind = AHEAD_NONE;
         int rc = ad_head_logits(m, m->cfg.n_layers, row(0), n, m->final_logits, stream);
+        const ad_filter *f = filter_at(temperature);
         if (rc == AD_OK)
-            rc = ad_verify_sampled_wait(m, m->final_logits, m->draft_logits, draft, n, temperature, u_accept, u_resample, u_final, n_accept, next,
-                                        ratio, stream);
+            rc = f ? ad_verify_filtered_wait(m, m->final_logits, m->draft_logits, draft, n, f, u_accept, u_resample, u_final, n_accept, next, ratio, stream)
+                   : ad_verify_sampled_wait(m, m->final_logits, m->draft_logits, draft, n, temperature, u_accept, u_resample, u_final, n_accept, next,
+                                            ratio, stream);
         if (rc != AD_OK) return rc;
         if ((rc = fused_health(m, stream))) return rc;
         const int64_t s = m->cfg.dtype == AD_F32 ? 4 : 2;
@@ -1294,9 +1399,9 @@ struct GpuBackend : Backend {
 
 }  // namespace
 
-ad_status ad_generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *gp,
-                      int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
-                      int64_t *n_events, void *stream) {
+static ad_status generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *gp, const ad_filter *filter,
+                          int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
+                          int64_t *n_events, void *stream) {
     if (!m || !kv || !prompt || !gp || !out_tokens || !n_out) return (ad_status)fail(AD_EINVAL, "ad_generate: null argument");
     if (kv->model != m) return (ad_status)fail(AD_EINVAL, "ad_generate: cache belongs to another model");
     if (n_prompt < 1 || gp->max_new < 1) return (ad_status)fail(AD_EINVAL, "ad_generate: empty prompt or max_new < 1");
@@ -1313,6 +1418,7 @@ ad_status ad_generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32
     for (int i = 0; i < AD_MAX_EXIT; ++i) sc.exit_layers[i] = m->cfg.exit_layers[i];
     GpuBackend be;
     be.m = m; be.kv = kv; be.stream = stream;
+    if (filter) be.filter = *filter;
     int rc = run_algorithm1(be, sc, *gp, prompt, n_prompt, out_tokens, n_out, stats, events, max_events, n_events);
     if (stats) stats->bytes_algorithmic = be.bytes;
     // nothing the call enqueued (work issued ahead of an outcome included) is still running when it returns
@@ -1320,6 +1426,24 @@ ad_status ad_generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32
     if (rc == AD_OK && (rc = stream_sync(stream))) return (ad_status)hip_fail(rc, "ad_generate");
     if (rc == AD_OK) rc = fused_health(m, stream);
     return (ad_status)rc;
+}
+
+ad_status ad_generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *gp,
+                      int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
+                      int64_t *n_events, void *stream) {
+    return generate(m, kv, prompt, n_prompt, gp, nullptr, out_tokens, n_out, stats, events, max_events, n_events, stream);
+}
+
+ad_status ad_generate_filtered(const ad_model *m, ad_kv *kv, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *gp,
+                               const ad_filter *f, int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events,
+                               int64_t max_events, int64_t *n_events, void *stream) {
+    if (!m || !gp || !f) return (ad_status)fail(AD_EINVAL, "ad_generate_filtered: null argument");
+    FilterArgs a;
+    const int rc = filter_args(m, f, a, "ad_generate_filtered");
+    if (rc) return (ad_status)rc;
+    ad_gen_params p = *gp;
+    p.temperature = f->temperature;
+    return generate(m, kv, prompt, n_prompt, &p, f, out_tokens, n_out, stats, events, max_events, n_events, stream);
 }
 
 }  // extern "C"
