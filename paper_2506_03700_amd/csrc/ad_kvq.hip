@@ -237,9 +237,12 @@ __global__ void __launch_bounds__(256) k_kvq_expand(KvqExpand a) {
 // dealt out the same way.  Rows of the four score tiles are assigned to keys so that lane (n, gq) ends up with keys gq * 16 .. + 15 of query row n, which is, eight by
 // eight, the B operand of O^T = V^T P^T against 16 consecutive positions of a dimension.  The scales never touch the codes: K's multiply the scores, V's the
 // probabilities, relative to the largest that the row has seen so that fp16 has them all in range (again hi and lo).
-template <int DH>
-struct KvqAttnLds {                                        // of one row tile at a time
-    float mx[kKvqWaves][16], sum[kKvqWaves][16];
+template <int DH, int RT>
+struct KvqAttnLds {
+    f16x8 q[RT][DH / 64][2][2][64];                        // [row tile][pair of k-steps][of the pair][hi, lo][lane]
+    float q_mul[RT * 16];
+    int see[RT * 16], tok[RT * 16];
+    float mx[kKvqWaves][16], sum[kKvqWaves][16];           // the wavefronts' results, one row tile at a time
     float part[kKvqWaves][16][DH + 4];                     // (rows padded to 16 bytes for 128-bit stores)
 };
 
@@ -276,7 +279,7 @@ template <int DH, int RT>
 __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
     constexpr int J = DH / 64, DT = DH / 16, RP = RT * 16, PR = DH + 2;
     constexpr int kPBits = 14;                             // probabilities times 2^14: those of 2^-17 and more keep 22 bits in fp16 hi and lo
-    __shared__ __attribute__((aligned(16))) KvqAttnLds<DH> L;
+    __shared__ __attribute__((aligned(16))) KvqAttnLds<DH, RT> L;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, gq = lane >> 4;
     const int item = blockIdx.x, g = quotient(item, a.S, a.mul_S), s = item - g * a.S;
     const int b_end = (a.n + kKvqBlock - 1) / kKvqBlock, b0 = s * a.per, b1 = b0 + a.per < b_end ? b0 + a.per : b_end;
@@ -306,52 +309,59 @@ __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
             load_k(b);
             load_v(b);
         }
-        // queries, each lane its own part; rows past the last are zeros
-        f16x8 q[RT][J][2][2];                              // [.][k-step of the pair][hi, lo]
-        float q_mul[RT], mx[RT], sum[RT];
-        int t_row[RT], see[RT], e_ref[RT];                 // o is in units of 2^(e_ref - 127 - kPBits)
-        f32x4 o[RT][DT];
+        // queries: a thread takes 16 dimensions of a row; rows past the last are zeros
+        constexpr int LR = DH / 16;                        // threads per row
+        for (int idx = tid; idx < RP * LR; idx += 256) {
+            const int rr = idx / LR, ch = idx % LR, r = r0 + (rr < nr ? rr : 0), t = quotient(r, a.G, a.mul_G), hq = g * a.G + (r - t * a.G);
+            const float *qp = a.q + (size_t)t * a.ld_q + (size_t)hq * DH + ch * 16;
+            f32x4 x[4];
+            float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int rr = i * 16 + n, r = r0 + (rr < nr ? rr : 0), t = quotient(r, a.G, a.mul_G), hq = g * a.G + (r - t * a.G);
-            const float *qp = a.q + (size_t)t * a.ld_q + (size_t)hq * DH + gq * 16;
-            float x[J][16], m = 0.f;
+            for (int e = 0; e < 4; ++e) {
+                x[e] = *(const f32x4 *)(qp + e * 4);
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x4 w = *(const f32x4 *)(qp + j * 64 + e * 4);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        x[j][e * 4 + c] = rr < nr ? w[c] : 0.f;
-                        m = fmaxf(m, finite_abs(x[j][e * 4 + c]));
-                    }
+                for (int c = 0; c < 4; ++c) {
+                    x[e][c] = rr < nr ? x[e][c] : 0.f;
+                    m = fmaxf(m, finite_abs(x[e][c]));
                 }
-            m = max_rows(m);
+            }
+            m = fmaxf(m, dpp<0xB1>(m));                    // over the row's 4 or 8 neighbouring lanes
+            m = fmaxf(m, dpp<0x4E>(m));
+            if (LR == 8) m = fmaxf(m, dpp<0x141>(m));
             // 2^(7 - exponent of m): both it and its inverse stay normal numbers
             int ex = (int)(__float_as_uint(m) >> 23) - 127;
             ex = ex < -100 ? -100 : ex;
             const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
-            q_mul[i] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale;
-            t_row[i] = t;
-            see[i] = a.see[0];
 #pragma unroll
-            for (int c = 1; c < 8; ++c) see[i] = t == c ? a.see[c] : see[i];
+            for (int h = 0; h < 2; ++h) {
+                u16x8 hi8, lo8;
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u16x8 hi8, lo8;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        uint16_t hi, lo;
-                        split16<true>(x[j][h * 8 + e] * up, hi, lo);
-                        hi8[e] = hi;
-                        lo8[e] = lo;
-                    }
-                    q[i][j][h][0] = __builtin_bit_cast(f16x8, hi8);
-                    q[i][j][h][1] = __builtin_bit_cast(f16x8, lo8);
+                for (int e = 0; e < 8; ++e) {
+                    uint16_t hi, lo;
+                    split16<true>(x[h * 2 + (e >> 2)][e & 3] * up, hi, lo);
+                    hi8[e] = hi;
+                    lo8[e] = lo;
                 }
+                L.q[rr >> 4][ch >> 2][h][0][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, hi8);
+                L.q[rr >> 4][ch >> 2][h][1][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, lo8);
+            }
+            if (ch == 0) {
+                L.q_mul[rr] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale;
+                int see = a.see[0];
+#pragma unroll
+                for (int c = 1; c < 8; ++c) see = t == c ? a.see[c] : see;
+                L.see[rr] = see;
+                L.tok[rr] = t;
+            }
+        }
+        __syncthreads();
+        float q_mul[RT], mx[RT], sum[RT];
+        int see[RT], e_ref[RT];                            // o is in units of 2^(e_ref - 127 - kPBits)
+        f32x4 o[RT][DT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            q_mul[i] = L.q_mul[i * 16 + n];
+            see[i] = L.see[i * 16 + n];
             mx[i] = -INFINITY;
             sum[i] = 0.f;
             e_ref[i] = 0;
@@ -364,20 +374,28 @@ __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
             const bool part_hidden = p0 + kKvqBlock > a.n_all;         // some row does not see all of the block
             f32x4 sc[RT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int i = 0; i < RT; ++i) sc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < 4; ++t) sc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < J; ++j)
+            for (int j = 0; j < J; ++j)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 2; ++h) {
+                    f16x8 q[RT][2];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) q[i][x] = L.q[i][j][h][x][lane];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
                         const f16x8 kk = operand(k[t][j][2 * h], k[t][j][2 * h + 1]);
 #pragma unroll
-                        for (int i = 0; i < RT; ++i)
+                        for (int x = 0; x < 2; ++x)
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) sc[i][t] = mma(kk, q[i][j][h][x], sc[i][t]);
+                            for (int i = 0; i < RT; ++i) sc[i][t] = mma(kk, q[i][x], sc[i][t]);
                     }
-            }
+                    __builtin_amdgcn_sched_barrier(0);     // (all conversions at once would take twice the registers)
+                }
             float k_mul[16];
 #pragma unroll
             for (int c = 0; c < 16; ++c) k_mul[c] = two_to((ks[c >> 2] >> (8 * (c & 3))) & 0xffu);
@@ -430,21 +448,21 @@ __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
                 mx[i] = nm;
                 float add = 0.f;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u16x8 hi8, lo8;
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < 8; e += 2) {
                         const int c = h * 8 + e;
-                        const float x = exp2_fast(w[c] - ref);
-                        add += x;
-                        uint16_t hi, lo;
-                        split16<true>(ldexpf(x, vb[c] - e_new + kPBits), hi, lo);
-                        hi8[e] = hi;
-                        lo8[e] = lo;
+                        const float x0 = exp2_fast(w[c] - ref), x1 = exp2_fast(w[c + 1] - ref);
+                        add += x0 + x1;
+                        const float y0 = ldexpf(x0, vb[c] - e_new + kPBits), y1 = ldexpf(x1, vb[c + 1] - e_new + kPBits);
+                        // (both parts cut off, two values an instruction: what is lost is below 2^-21 of the value)
+                        const auto hi = __builtin_amdgcn_cvt_pkrtz(y0, y1);
+                        const auto lo = __builtin_amdgcn_cvt_pkrtz(y0 - (float)hi[0], y1 - (float)hi[1]);
+                        p[i][h][0][e] = (_Float16)hi[0];
+                        p[i][h][0][e + 1] = (_Float16)hi[1];
+                        p[i][h][1][e] = (_Float16)lo[0];
+                        p[i][h][1][e + 1] = (_Float16)lo[1];
                     }
-                    p[i][h][0] = __builtin_bit_cast(f16x8, hi8);
-                    p[i][h][1] = __builtin_bit_cast(f16x8, lo8);
-                }
                 sum[i] = sum[i] * alpha + add;
                 const float f = alpha * shrink;
                 if (!__all(f == 1.0f)) {
@@ -464,31 +482,35 @@ __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
                     }
             }
             if (part_hidden && __any(bad)) {
+#pragma unroll 1
                 for (int t = 0; t < a.m; ++t) {
                     const int l0 = a.see[t] + 1 - p0 - gq * 16;
+                    u32x4 keep;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d)
+                    for (int w = 0; w < 4; ++w) {
+                        const int l = l0 - 4 * w;
+                        keep[w] = l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u;
+                    }
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t w[2];
+                    for (int i = 0; i < RT; ++i) {
+                        const bool mine = L.tok[i * 16 + n] == t;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int l = l0 - 4 * (2 * h + e);
-                                w[e] = v[d][2 * h + e] & (l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u);
-                            }
-                            const f16x8 vv = operand(w[0], w[1]);
+                        for (int d = 0; d < DT; ++d) {
+                            f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int i = 0; i < RT; ++i) {
-                                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                            for (int h = 0; h < 2; ++h) {
+                                const f16x8 vv = operand(v[d][2 * h] & keep[2 * h], v[d][2 * h + 1] & keep[2 * h + 1]);
                                 x = mma(vv, p[i][h][0], x);
                                 x = mma(vv, p[i][h][1], x);
-                                if (t_row[i] == t) o[i][d] += x;
                             }
+                            if (mine) o[i][d] += x;
+                            __builtin_amdgcn_sched_barrier(0);         // (rare: as few registers as it takes)
                         }
+                    }
                 }
             } else {
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
+                for (int d = 0; d < DT; ++d) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const f16x8 vv = operand(v[d][2 * h], v[d][2 * h + 1]);
@@ -497,6 +519,8 @@ __global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
 #pragma unroll
                             for (int x = 0; x < 2; ++x) o[i][d] = mma(vv, p[i][h][x], o[i][d]);
                     }
+                    if (d & 1) __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if (b + kKvqWaves < b1) load_v(b + kKvqWaves);
         }
@@ -645,8 +669,8 @@ int launch_kvq_expand(const KvqExpand &a, const LaunchCtx &c) {
     return (int)hipErrorInvalidValue;
 }
 
-// Items: one per compute unit, but no fewer blocks than an item has wavefronts; contexts of up to two blocks per wavefront are one item
-// per kv head, which writes the output itself.
+// Blocks per item: as many as it has wavefronts, or the smallest multiple of that for which the items are no more than the compute units; contexts of up to
+// two blocks per wavefront are one item per kv head, which writes the output itself.
 void kvq_attn_finish(KvqAttn &a, int n_wg) {
     a.G = a.Hq / a.c.Hkv;
     a.R = a.G * a.m;
@@ -656,11 +680,15 @@ void kvq_attn_finish(KvqAttn &a, int n_wg) {
         a.n_all = a.see[t] + 1 < a.n_all ? a.see[t] + 1 : a.n_all;
     }
     const int blocks = (a.n + kKvqBlock - 1) / kKvqBlock;
-    int S = n_wg / a.c.Hkv;
-    if (S > blocks / kKvqWaves) S = blocks / kKvqWaves;
-    if (S > kKvqMaxSplits) S = kKvqMaxSplits;
-    if (S < 1 || blocks <= 2 * kKvqWaves) S = 1;
-    a.per = (blocks + S - 1) / S;
+    a.per = kKvqWaves;
+    if (blocks <= 2 * kKvqWaves) {
+        a.per = 2 * kKvqWaves;
+    } else {
+        int most = n_wg / a.c.Hkv;                       // items per kv head
+        most = most < 1 ? 1 : most > kKvqMaxSplits ? kKvqMaxSplits : most;
+        const int least = (blocks + most - 1) / most;
+        if (least > a.per) a.per = (least + kKvqWaves - 1) / kKvqWaves * kKvqWaves;
+    }
     a.S = (blocks + a.per - 1) / a.per;
     a.mul_S = div_multiplier(a.S);
     a.mul_G = div_multiplier(a.G);
