@@ -16,7 +16,6 @@
 namespace ad {
 
 constexpr int kKvqBlock = 64;            // positions per block of V, and per step of the attention kernel
-constexpr int kKvqWaves = 4;             // wavefronts per workgroup of the attention kernel
 constexpr int kKvqMaxSplits = 512;       // most work items of a kv head
 
 struct KvqCache {
@@ -67,7 +66,7 @@ struct KvqAttn {
     int m, Hq, G, R;                     // tokens, query heads, those per kv head, query rows per kv head
     int see[8];                          // last position that token t's queries see
     int n, n_all;                        // positions that some row sees, that all rows see
-    int S, per;                          // work items per kv head, blocks of 64 positions per item
+    int S, per, waves, tiles;            // work items per kv head, blocks of 64 positions and wavefronts per item, tiles of 16 query rows per workgroup
     unsigned mul_S, mul_G, mul_R;
     float scale;                         // of the scores, in powers of two: log2(e) / sqrt(head_dim)
     float *part;                         // [Hkv][S][R][dh + 2]

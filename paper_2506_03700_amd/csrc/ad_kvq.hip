@@ -2,6 +2,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "ad_device.h"
 #include "ad_internal.h"
 #include "ad_kvq.h"
@@ -229,21 +231,29 @@ __global__ void __launch_bounds__(256) k_kvq_expand(KvqExpand a) {
 // ---------------------------------------------------------------------------------------------------
 // attention
 // ---------------------------------------------------------------------------------------------------
-// Work item (kv head, split): a workgroup of four wavefronts that take the item's blocks of 64 positions in turn, under an online softmax of their
-// own; their results meet in LDS, the items' in k_kvq_combine.  All query rows of the kv head's group meet a block's codes while they are in registers.
+// Work item (kv head, split): a workgroup whose wavefronts take the item's blocks of 64 positions in turn, under an online softmax of their
+// own; their results meet in LDS, the items' in k_kvq_combine.  All of a pass's query rows (16 or 32) of the kv head's group meet a block's codes.
 //
 // Products.  S^T = K q^T: codes are exact in fp16, queries are scaled to a largest magnitude in [128, 256) and split into fp16 hi and lo parts (22 bits), sums are
-// fp32.  A lane loads 16 consecutive dimensions of a key: the first eight are its part of one k-step, the other eight of the next, and the queries are
+// fp32.  A lane has 16 consecutive dimensions of a key: the first eight are its part of one k-step, the other eight of the next, and the queries are
 // dealt out the same way.  Rows of the four score tiles are assigned to keys so that lane (n, gq) ends up with keys gq * 16 .. + 15 of query row n, which is, eight by
 // eight, the B operand of O^T = V^T P^T against 16 consecutive positions of a dimension.  The scales never touch the codes: K's multiply the scores, V's the
 // probabilities, relative to the largest that the row has seen so that fp16 has them all in range (again hi and lo).
-template <int DH, int RT>
+//
+// Copies.  Every wavefront has room for one block's codes in LDS, filled from memory without a way through registers and in operand order: the next block's
+// K is on its way as soon as the scores are formed, its V after the second product, and nobody else reads or writes there, so the loop has no barriers.
+template <int DH, int RT, int NW>
 struct KvqAttnLds {
+    static constexpr int KU = DH / 64 * 4 * 64, VU = DH / 16 * 64;      // 16-byte units of a block: [tile][pair of k-steps][lane], [16 dimensions][lane]
+    union {
+        u32x4 codes[NW][KU + VU];
+        float part[NW][16][DH + 4];                        // the wavefronts' results, one row tile at a time (rows padded to 16 bytes)
+    };
+    u32x4 scales[NW][16];                                  // 64 bytes of K's, 64 of V's (and the same again)
     f16x8 q[RT][DH / 64][2][2][64];                        // [row tile][pair of k-steps][of the pair][hi, lo][lane]
     float q_mul[RT * 16];
     int see[RT * 16], tok[RT * 16];
-    float mx[kKvqWaves][16], sum[kKvqWaves][16];           // the wavefronts' results, one row tile at a time
-    float part[kKvqWaves][16][DH + 4];                     // (rows padded to 16 bytes for 128-bit stores)
+    float mx[NW][16], sum[NW][16];
 };
 
 // x / d for any x >= 0: the rounded-up reciprocal is never too small and, below 2^32, at most one too large
@@ -275,293 +285,328 @@ __device__ __forceinline__ void kvq_output(const KvqAttn &a, int g, int r, int d
     }
 }
 
-template <int DH, int RT>
-__global__ void __launch_bounds__(256, RT == 1 ? 2 : 1) k_kvq_attn(KvqAttn a) {
-    constexpr int J = DH / 64, DT = DH / 16, RP = RT * 16, PR = DH + 2;
-    constexpr int kPBits = 14;                             // probabilities times 2^14: those of 2^-17 and more keep 22 bits in fp16 hi and lo
-    __shared__ __attribute__((aligned(16))) KvqAttnLds<DH, RT> L;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, gq = lane >> 4;
+// waits until at most N copies are in flight and what has been read from LDS is there
+template <int N>
+__device__ __forceinline__ void copies_left() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4 << 14));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// lane l's 16 bytes, 4 bytes go to place l of dst (the same for all lanes)
+__device__ __forceinline__ void units_to_lds(const void *src, void *dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void words_to_lds(const void *src, void *dst) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src, (__attribute__((address_space(3))) void *)dst, 4, 0, 0);
+}
+
+template <int DH, int RT, int NW>
+__global__ void __launch_bounds__(64 * NW, NW / 4) k_kvq_attn(KvqAttn a) {
+    constexpr int J = DH / 64, DT = DH / 16, RP = RT * 16, PR = DH + 2, NTH = 64 * NW, KU = KvqAttnLds<DH, RT, NW>::KU;
+    constexpr int NK = 4 * J + 1, NV = DT;                 // copies of a block's K (with the scales), of its V
+    constexpr int kPBits = 14;                             // probabilities times 2^14: those of 2^-17 and more keep 21 bits in fp16 hi and lo
+    extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+    KvqAttnLds<DH, RT, NW> &L = *reinterpret_cast<KvqAttnLds<DH, RT, NW> *>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, gq = lane >> 4;
     const int item = blockIdx.x, g = quotient(item, a.S, a.mul_S), s = item - g * a.S;
+    const int r0 = blockIdx.y * RP, nr = a.R - r0 < RP ? a.R - r0 : RP;
     const int b_end = (a.n + kKvqBlock - 1) / kKvqBlock, b0 = s * a.per, b1 = b0 + a.per < b_end ? b0 + a.per : b_end;
     const uint8_t *Kg = a.c.Kc + (size_t)g * a.c.stride * DH, *Vg = a.c.Vc + (size_t)g * a.c.stride * DH;
-    const uint8_t *Ksg = a.c.Ks + (size_t)g * a.c.stride, *Vsg = a.c.Vs + (size_t)g * a.c.stride;
-
-    u32x4 k[4][J], v[DT], ks, vs;
-    auto load_k = [&](int b) {
+    const uint8_t *Sg = ((lane & 31) < 16 ? a.c.Ks : a.c.Vs) + (size_t)g * a.c.stride + (lane & 15) * 4;
+    u32x4 *const my = L.codes[wave];
+    auto copy_k = [&](int b) {
         const uint8_t *base = Kg + (size_t)b * kKvqBlock * DH + ((n >> 2) * 16 + (n & 3)) * DH + gq * 16;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int j = 0; j < J; ++j) k[t][j] = *(const u32x4 *)(base + t * 4 * DH + j * 64);
-        ks = *(const u32x4 *)(Ksg + (size_t)b * kKvqBlock + gq * 16);
+            for (int j = 0; j < J; ++j) units_to_lds(base + t * 4 * DH + j * 64, my + (t * J + j) * 64);
+        words_to_lds(Sg + (size_t)b * kKvqBlock, &L.scales[wave][0]);
     };
-    auto load_v = [&](int b) {
+    auto copy_v = [&](int b) {
         const uint8_t *base = Vg + (size_t)b * kKvqBlock * DH + n * kKvqBlock + gq * 16;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) v[d] = *(const u32x4 *)(base + d * 16 * kKvqBlock);
-        vs = *(const u32x4 *)(Vsg + (size_t)b * kKvqBlock + gq * 16);
+        for (int d = 0; d < DT; ++d) units_to_lds(base + d * 16 * kKvqBlock, my + KU + d * 64);
     };
-
-    for (int r0 = 0; r0 < a.R; r0 += RP) {
-        const int nr = a.R - r0 < RP ? a.R - r0 : RP;
-        int b = b0 + wave;
-        if (b < b1) {
-            load_k(b);
-            load_v(b);
-        }
-        // queries: a thread takes 16 dimensions of a row; rows past the last are zeros
-        constexpr int LR = DH / 16;                        // threads per row
-        for (int idx = tid; idx < RP * LR; idx += 256) {
-            const int rr = idx / LR, ch = idx % LR, r = r0 + (rr < nr ? rr : 0), t = quotient(r, a.G, a.mul_G), hq = g * a.G + (r - t * a.G);
-            const float *qp = a.q + (size_t)t * a.ld_q + (size_t)hq * DH + ch * 16;
-            f32x4 x[4];
-            float m = 0.f;
+    // queries: a thread takes 16 dimensions of a row; rows past the last are zeros.  Their loads come before the copies: what waits for them does not wait for those.
+    constexpr int LR = DH / 16;                            // threads per row
+    static_assert(RP * LR <= NTH, "a turn for all rows");
+    const int rr = tid / LR, ch = tid % LR, r_q = r0 + (rr < nr ? rr : 0), t_q = quotient(r_q, a.G, a.mul_G);
+    f32x4 x[4];
+    if (tid < RP * LR) {
+        const float *qp = a.q + (size_t)t_q * a.ld_q + (size_t)(g * a.G + (r_q - t_q * a.G)) * DH + ch * 16;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = *(const f32x4 *)(qp + e * 4);
+        for (int e = 0; e < 4; ++e) x[e] = *(const f32x4 *)(qp + e * 4);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    int b = b0 + wave;
+    if (b < b1) {
+        copy_k(b);
+        copy_v(b);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (tid < RP * LR) {
+        float m = 0.f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    x[e][c] = rr < nr ? x[e][c] : 0.f;
-                    m = fmaxf(m, finite_abs(x[e][c]));
-                }
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[e][c] = rr < nr ? x[e][c] : 0.f;
+                m = fmaxf(m, finite_abs(x[e][c]));
             }
-            m = fmaxf(m, dpp<0xB1>(m));                    // over the row's 4 or 8 neighbouring lanes
-            m = fmaxf(m, dpp<0x4E>(m));
-            if (LR == 8) m = fmaxf(m, dpp<0x141>(m));
-            // 2^(7 - exponent of m): both it and its inverse stay normal numbers
-            int ex = (int)(__float_as_uint(m) >> 23) - 127;
-            ex = ex < -100 ? -100 : ex;
-            const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+        m = fmaxf(m, dpp<0xB1>(m));                        // over the row's 4 or 8 neighbouring lanes
+        m = fmaxf(m, dpp<0x4E>(m));
+        if (LR == 8) m = fmaxf(m, dpp<0x141>(m));
+        // 2^(7 - exponent of m): both it and its inverse stay normal numbers
+        int ex = (int)(__float_as_uint(m) >> 23) - 127;
+        ex = ex < -100 ? -100 : ex;
+        const float up = __uint_as_float((uint32_t)(127 + 7 - ex) << 23);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u16x8 hi8, lo8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint16_t hi, lo;
+                split16<true>(x[h * 2 + (e >> 2)][e & 3] * up, hi, lo);
+                hi8[e] = hi;
+                lo8[e] = lo;
+            }
+            L.q[rr >> 4][ch >> 2][h][0][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, hi8);
+            L.q[rr >> 4][ch >> 2][h][1][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, lo8);
+        }
+        if (ch == 0) {
+            L.q_mul[rr] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale;
+            int see = a.see[0];
+#pragma unroll
+            for (int c = 1; c < 8; ++c) see = t_q == c ? a.see[c] : see;
+            L.see[rr] = see;
+            L.tok[rr] = t_q;
+        }
+    }
+    // (a barrier that leaves the copies in flight)
+    copies_left<63>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    float q_mul[RT], mx[RT], sum[RT];
+    int see[RT], e_ref[RT];                                // o is in units of 2^(e_ref - 127 - kPBits)
+    f32x4 o[RT][DT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        q_mul[i] = L.q_mul[i * 16 + n];
+        see[i] = L.see[i * 16 + n];
+        mx[i] = -INFINITY;
+        sum[i] = 0.f;
+        e_ref[i] = 0;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[i][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (; b < b1; b += NW) {
+        const int p0 = b * kKvqBlock, next = b + NW;
+        const bool part_hidden = p0 + kKvqBlock > a.n_all;             // some row does not see all of the block
+        copies_left<NV>();
+        f32x4 sc[RT][4];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        const u32x4 ks = L.scales[wave][gq];
+        u32x4 vs = L.scales[wave][4 + gq];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            u32x4 k[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) k[t] = my[(t * J + j) * 64 + lane];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                u16x8 hi8, lo8;
+                f16x8 q[RT][2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    uint16_t hi, lo;
-                    split16<true>(x[h * 2 + (e >> 2)][e & 3] * up, hi, lo);
-                    hi8[e] = hi;
-                    lo8[e] = lo;
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) q[i][x] = L.q[i][j][h][x][lane];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const f16x8 kk = operand(k[t][2 * h], k[t][2 * h + 1]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) sc[i][t] = mma(kk, q[i][x], sc[i][t]);
                 }
-                L.q[rr >> 4][ch >> 2][h][0][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, hi8);
-                L.q[rr >> 4][ch >> 2][h][1][(rr & 15) + 16 * (ch & 3)] = __builtin_bit_cast(f16x8, lo8);
-            }
-            if (ch == 0) {
-                L.q_mul[rr] = __uint_as_float((uint32_t)(127 - 7 + ex) << 23) * a.scale;
-                int see = a.see[0];
-#pragma unroll
-                for (int c = 1; c < 8; ++c) see = t == c ? a.see[c] : see;
-                L.see[rr] = see;
-                L.tok[rr] = t;
             }
         }
-        __syncthreads();
-        float q_mul[RT], mx[RT], sum[RT];
-        int see[RT], e_ref[RT];                            // o is in units of 2^(e_ref - 127 - kPBits)
-        f32x4 o[RT][DT];
+        if (next < b1) {
+            copies_left<NV>();                             // (what has been read of K is there: its place is free)
+            copy_k(next);
+        }
+        // entries behind the last position that is seen may be anything: their codes and scales are taken out
+        const int live = a.n - p0 - gq * 16;               // of this lane's 16 positions
+        const bool ragged = p0 + kKvqBlock > a.n;
+        u32x4 keep = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+        auto keep_first = [&](int count) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int l = count - 4 * w;
+                keep[w] = l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u;
+            }
+        };
+        if (ragged) {
+            keep_first(live);
+            vs &= keep;
+        }
+        float k_mul[16];
+        int vb[16], top = 0;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            k_mul[c] = two_to((ks[c >> 2] >> (8 * (c & 3))) & 0xffu);
+            vb[c] = (int)((vs[c >> 2] >> (8 * (c & 3))) & 0xffu);
+            top = vb[c] > top ? vb[c] : top;
+        }
+        f16x8 p[RT][2][2];                                 // [.][k-step][hi, lo]
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            q_mul[i] = L.q_mul[i * 16 + n];
-            see[i] = L.see[i * 16 + n];
-            mx[i] = -INFINITY;
-            sum[i] = 0.f;
-            e_ref[i] = 0;
+            float w[16], bm = -INFINITY;
+            int e_new = top;
+            if (part_hidden) {                             // (what a row does not see has no part in its scale)
+                e_new = 0;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[i][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        }
-
-        for (; b < b1; b += kKvqWaves) {
-            const int p0 = b * kKvqBlock;
-            const bool part_hidden = p0 + kKvqBlock > a.n_all;         // some row does not see all of the block
-            f32x4 sc[RT][4];
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) sc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    f16x8 q[RT][2];
-#pragma unroll
-                    for (int i = 0; i < RT; ++i)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) q[i][x] = L.q[i][j][h][x][lane];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const f16x8 kk = operand(k[t][j][2 * h], k[t][j][2 * h + 1]);
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)
-#pragma unroll
-                            for (int i = 0; i < RT; ++i) sc[i][t] = mma(kk, q[i][x], sc[i][t]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);     // (all conversions at once would take twice the registers)
-                }
-            float k_mul[16];
-#pragma unroll
-            for (int c = 0; c < 16; ++c) k_mul[c] = two_to((ks[c >> 2] >> (8 * (c & 3))) & 0xffu);
-            if (b + kKvqWaves < b1) load_k(b + kKvqWaves);
-            // entries behind the last position that is seen may be anything: their codes and scales are taken out
-            const int live = a.n - p0 - gq * 16;                       // of this lane's 16 positions
-            if (live < 16) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int l = live - 4 * w;
-                    const uint32_t keep = l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u;
-                    vs[w] &= keep;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) v[d][w] &= keep;
-                }
-            }
-            int vb[16], top = 0;
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-                vb[c] = (int)((vs[c >> 2] >> (8 * (c & 3))) & 0xffu);
-                top = vb[c] > top ? vb[c] : top;
-            }
-            f16x8 p[RT][2][2];                             // [.][k-step][hi, lo]
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                float w[16], bm = -INFINITY;
-                int e_new = top;
-                if (part_hidden) {                         // (what a row does not see has no part in its scale)
-                    e_new = 0;
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const bool seen = p0 + gq * 16 + c <= see[i];
-                        w[c] = seen ? sc[i][c >> 2][c & 3] * q_mul[i] * k_mul[c] : -INFINITY;
-                        e_new = seen && vb[c] > e_new ? vb[c] : e_new;
-                        bm = fmaxf(bm, w[c]);
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        w[c] = sc[i][c >> 2][c & 3] * q_mul[i] * k_mul[c];
-                        bm = fmaxf(bm, w[c]);
-                    }
-                }
-                bm = max_rows(bm);
-                e_new = (int)max_rows((float)e_new);
-                e_new = e_new > e_ref[i] ? e_new : e_ref[i];
-                const float shrink = ldexpf(1.0f, e_ref[i] - e_new);
-                e_ref[i] = e_new;
-                const float nm = fmaxf(mx[i], bm), ref = softmax_ref(nm), alpha = exp2_fast(mx[i] - ref);
-                mx[i] = nm;
-                float add = 0.f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const int c = h * 8 + e;
-                        const float x0 = exp2_fast(w[c] - ref), x1 = exp2_fast(w[c + 1] - ref);
-                        add += x0 + x1;
-                        const float y0 = ldexpf(x0, vb[c] - e_new + kPBits), y1 = ldexpf(x1, vb[c + 1] - e_new + kPBits);
-                        // (both parts cut off, two values an instruction: what is lost is below 2^-21 of the value)
-                        const auto hi = __builtin_amdgcn_cvt_pkrtz(y0, y1);
-                        const auto lo = __builtin_amdgcn_cvt_pkrtz(y0 - (float)hi[0], y1 - (float)hi[1]);
-                        p[i][h][0][e] = (_Float16)hi[0];
-                        p[i][h][0][e + 1] = (_Float16)hi[1];
-                        p[i][h][1][e] = (_Float16)lo[0];
-                        p[i][h][1][e + 1] = (_Float16)lo[1];
-                    }
-                sum[i] = sum[i] * alpha + add;
-                const float f = alpha * shrink;
-                if (!__all(f == 1.0f)) {
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[i][d] *= f;
-                }
-            }
-            // a value that is not a number, at a position that only some rows see, must not reach the others by way of 0 * NaN
-            bool bad = false;
-            if (part_hidden) {
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const uint32_t x = (v[d][w] & 0x7f7f7f7fu) + 0x01010101u;
-                        bad |= (x & 0x80808080u) != 0;
-                    }
-            }
-            if (part_hidden && __any(bad)) {
-#pragma unroll 1
-                for (int t = 0; t < a.m; ++t) {
-                    const int l0 = a.see[t] + 1 - p0 - gq * 16;
-                    u32x4 keep;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int l = l0 - 4 * w;
-                        keep[w] = l >= 4 ? 0xffffffffu : l <= 0 ? 0u : (1u << (8 * l)) - 1u;
-                    }
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        const bool mine = L.tok[i * 16 + n] == t;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const f16x8 vv = operand(v[d][2 * h] & keep[2 * h], v[d][2 * h + 1] & keep[2 * h + 1]);
-                                x = mma(vv, p[i][h][0], x);
-                                x = mma(vv, p[i][h][1], x);
-                            }
-                            if (mine) o[i][d] += x;
-                            __builtin_amdgcn_sched_barrier(0);         // (rare: as few registers as it takes)
-                        }
-                    }
+                for (int c = 0; c < 16; ++c) {
+                    const bool seen = p0 + gq * 16 + c <= see[i];
+                    w[c] = seen ? sc[i][c >> 2][c & 3] * k_mul[c] : -INFINITY;
+                    e_new = seen && vb[c] > e_new ? vb[c] : e_new;
+                    bm = fmaxf(bm, w[c]);
                 }
             } else {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
+                for (int c = 0; c < 16; ++c) {
+                    w[c] = sc[i][c >> 2][c & 3] * k_mul[c];
+                    bm = fmaxf(bm, w[c]);
+                }
+            }
+            bm = max_rows(bm);
+            e_new = (int)max_rows((float)e_new);
+            e_new = e_new > e_ref[i] ? e_new : e_ref[i];
+            const float shrink = ldexpf(1.0f, e_ref[i] - e_new);
+            e_ref[i] = e_new;
+            const float nm = fmaxf(mx[i], bm * q_mul[i]), ref = softmax_ref(nm), alpha = exp2_fast(mx[i] - ref);
+            mx[i] = nm;
+            float add = 0.f;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const f16x8 vv = operand(v[d][2 * h], v[d][2 * h + 1]);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int i = 0; i < RT; ++i)
+                for (int e = 0; e < 8; e += 2) {
+                    const int c = h * 8 + e;
+                    const float x0 = exp2_fast(fmaf(w[c], q_mul[i], -ref)), x1 = exp2_fast(fmaf(w[c + 1], q_mul[i], -ref));
+                    add += x0 + x1;
+                    const float y0 = ldexpf(x0, vb[c] - e_new + kPBits), y1 = ldexpf(x1, vb[c + 1] - e_new + kPBits);
+                    // (both parts cut off, two values an instruction: what is lost is below 2^-21 of the value)
+                    const auto hi = __builtin_amdgcn_cvt_pkrtz(y0, y1);
+                    const auto lo = __builtin_amdgcn_cvt_pkrtz(y0 - (float)hi[0], y1 - (float)hi[1]);
+                    p[i][h][0][e] = (_Float16)hi[0];
+                    p[i][h][0][e + 1] = (_Float16)hi[1];
+                    p[i][h][1][e] = (_Float16)lo[0];
+                    p[i][h][1][e + 1] = (_Float16)lo[1];
+                }
+            sum[i] = sum[i] * alpha + add;
+            const float f = alpha * shrink;
+            if (!__all(f == 1.0f)) {
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) o[i][d] = mma(vv, p[i][h][x], o[i][d]);
+                for (int d = 0; d < DT; ++d) o[i][d] *= f;
+            }
+        }
+        if (next < b1) copies_left<NK>();
+        else copies_left<0>();
+        // a value that is not a number, at a position that only some rows see, must not reach the others by way of 0 * NaN
+        bool bad = false;
+        if (part_hidden) {
+#pragma unroll 1
+            for (int d = 0; d < DT; ++d) {
+                const u32x4 v = my[KU + d * 64 + lane] & keep;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) bad |= (((v[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+            bad = __any(bad);
+        }
+        if (bad) {
+#pragma unroll 1
+            for (int t = 0; t < a.m; ++t) {
+                keep_first(a.see[t] + 1 - p0 - gq * 16);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const bool mine = L.tok[i * 16 + n] == t;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const u32x4 v = my[KU + d * 64 + lane] & keep;
+                        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const f16x8 vv = operand(v[2 * h], v[2 * h + 1]);
+                            x = mma(vv, p[i][h][0], x);
+                            x = mma(vv, p[i][h][1], x);
+                        }
+                        if (mine) o[i][d] += x;
+                        __builtin_amdgcn_sched_barrier(0);             // (rare: as few registers as it takes)
                     }
-                    if (d & 1) __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (b + kKvqWaves < b1) load_v(b + kKvqWaves);
+        } else {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                u32x4 v = my[KU + d * 64 + lane];
+                if (ragged) v &= keep;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f16x8 vv = operand(v[2 * h], v[2 * h + 1]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) o[i][d] = mma(vv, p[i][h][x], o[i][d]);
+                }
+            }
         }
-        // lane (n, gq): row n of a tile, dimensions d * 16 + gq * 4 .. + 3.  The wavefronts' results are folded in wavefront order.
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int ni = nr - i * 16 < 16 ? nr - i * 16 : 16;        // rows of this tile
-            if (ni <= 0) break;
-            const float den = sum_rows(sum[i]), unit = ldexpf(1.0f, e_ref[i] - 127 - kPBits);
-            if (gq == 0) {
-                L.mx[wave][n] = mx[i];
-                L.sum[wave][n] = den;
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) *(f32x4 *)&L.part[wave][n][d * 16 + gq * 4] = o[i][d] * unit;
-            __syncthreads();
-            for (int idx = tid; idx < ni * (DH / 2); idx += 256) {
-                const int rr = idx / (DH / 2), d = idx % (DH / 2) * 2, r = r0 + i * 16 + rr;
-                float M = -INFINITY, sums = 0.f;
-                f32x2 num = {0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < kKvqWaves; ++w) M = fmaxf(M, L.mx[w][rr]);
-                const float ref = softmax_ref(M);
-#pragma unroll
-                for (int w = 0; w < kKvqWaves; ++w) {
-                    const float f = exp2_fast(L.mx[w][rr] - ref);       // a wavefront without keys: exp(-inf) = 0, of sums that are 0
-                    const f32x2 x = *(const f32x2 *)&L.part[w][rr][d];
-                    sums += f * L.sum[w][rr];
-                    num[0] += f * x[0];
-                    num[1] += f * x[1];
-                }
-                if (a.S == 1) {
-                    kvq_output(a, g, r, d, num[0] / sums, num[1] / sums);
-                    continue;
-                }
-                float *out = a.part + (((size_t)g * a.S + s) * a.R + r) * PR;
-                *(f32x2 *)(out + d) = num;
-                if (d == 0) *(f32x2 *)(out + DH) = (f32x2){M, sums};
-            }
-            __syncthreads();
+        if (next < b1) {
+            copies_left<NK>();                             // (likewise V's)
+            copy_v(next);
         }
+    }
+    // lane (n, gq): row n of a tile, dimensions d * 16 + gq * 4 .. + 3.  The wavefronts' results are folded in wavefront order.
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int ni = nr - i * 16 < 16 ? nr - i * 16 : 16;            // rows of this tile
+        if (ni <= 0) break;
+        const float den = sum_rows(sum[i]), unit = ldexpf(1.0f, e_ref[i] - 127 - kPBits);
+        if (gq == 0) {
+            L.mx[wave][n] = mx[i];
+            L.sum[wave][n] = den;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4 *)&L.part[wave][n][d * 16 + gq * 4] = o[i][d] * unit;
+        __syncthreads();
+        for (int idx = tid; idx < ni * (DH / 2); idx += NTH) {
+            const int rr = idx / (DH / 2), d = idx % (DH / 2) * 2, r = r0 + i * 16 + rr;
+            float M = -INFINITY, sums = 0.f;
+            f32x2 num = {0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) M = fmaxf(M, L.mx[w][rr]);
+            const float ref = softmax_ref(M);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float f = exp2_fast(L.mx[w][rr] - ref);           // a wavefront without keys: exp(-inf) = 0, of sums that are 0
+                const f32x2 x = *(const f32x2 *)&L.part[w][rr][d];
+                sums += f * L.sum[w][rr];
+                num[0] += f * x[0];
+                num[1] += f * x[1];
+            }
+            if (a.S == 1) {
+                kvq_output(a, g, r, d, num[0] / sums, num[1] / sums);
+                continue;
+            }
+            float *out = a.part + (((size_t)g * a.S + s) * a.R + r) * PR;
+            *(f32x2 *)(out + d) = num;
+            if (d == 0) *(f32x2 *)(out + DH) = (f32x2){M, sums};
+        }
+        __syncthreads();
     }
 }
 
@@ -626,10 +671,36 @@ __global__ void __launch_bounds__(256) k_kvq_combine(KvqAttn a) {
     kvq_output(a, g, r, d, y[0] / sum, y[1] / sum);
 }
 
+// LDS beyond 64 KiB is asked for once per kernel and device, with that device current
+template <int DH, int RT, int NW>
+int allow_lds(int device) {
+    static std::atomic<uint64_t> done{0};
+    constexpr size_t lds = sizeof(KvqAttnLds<DH, RT, NW>);
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    int current = 0;
+    if (hipGetDevice(&current) != hipSuccess) return (int)hipGetLastError();
+    if (device < 0) device = current;
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return 0;
+    hipError_t e = device != current ? hipSetDevice(device) : hipSuccess;
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)k_kvq_attn<DH, RT, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (device != current) (void)hipSetDevice(current);
+    if (e == hipSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
+    return (int)e;
+}
+
+template <int DH, int RT, int NW>
+int launch_attn_as(const KvqAttn &a, const LaunchCtx &c) {
+    const int rc = allow_lds<DH, RT, NW>(c.device);
+    if (rc) return rc;
+    return launch<k_kvq_attn<DH, RT, NW>>(c, dim3(a.c.Hkv * a.S, (a.R + RT * 16 - 1) / (RT * 16)), dim3(64 * NW), sizeof(KvqAttnLds<DH, RT, NW>), a);
+}
+
 template <int DH>
 int launch_attn_dh(const KvqAttn &a, const LaunchCtx &c) {
-    const dim3 items(a.c.Hkv * a.S);
-    const int rc = a.R <= 16 ? launch<k_kvq_attn<DH, 1>>(c, items, dim3(256), 0, a) : launch<k_kvq_attn<DH, 2>>(c, items, dim3(256), 0, a);
+    int rc;
+    if (a.tiles == 1) rc = a.waves == 4 ? launch_attn_as<DH, 1, 4>(a, c) : launch_attn_as<DH, 1, 8>(a, c);
+    else rc = a.waves == 4 ? launch_attn_as<DH, 2, 4>(a, c) : launch_attn_as<DH, 2, 8>(a, c);
     if (rc || a.S == 1) return rc;
     return launch<k_kvq_combine<DH>>(c, dim3(a.c.Hkv * a.R), dim3(256), 0, a);
 }
@@ -669,8 +740,11 @@ int launch_kvq_expand(const KvqExpand &a, const LaunchCtx &c) {
     return (int)hipErrorInvalidValue;
 }
 
-// Blocks per item: as many as it has wavefronts, or the smallest multiple of that for which the items are no more than the compute units; contexts of up to
-// two blocks per wavefront are one item per kv head, which writes the output itself.
+// How the work is divided, for n_wg compute units.  A block of 64 positions per wavefront and 16 query rows per workgroup (the shortest chain) while every workgroup
+// has a compute unit to itself; else 32 rows, which a block's codes are converted once for, and beyond four blocks per compute unit 8 wavefronts and as many
+// blocks each as it takes.  Contexts of up to eight blocks are one item per kv head, which writes the output itself.
+// Measured, 32 query heads on 8 kv heads of 128 dimensions, 1 / 8 rows, us a call: context 300, 4 wavefronts 9.6 / 15.4, 8 8.9 / 13.1; 4096, 4 10.4 / 14.3, 8 11.5 / 15.9;
+// 9203 (both 8) 12.3 / 16.5.
 void kvq_attn_finish(KvqAttn &a, int n_wg) {
     a.G = a.Hq / a.c.Hkv;
     a.R = a.G * a.m;
@@ -680,14 +754,20 @@ void kvq_attn_finish(KvqAttn &a, int n_wg) {
         a.n_all = a.see[t] + 1 < a.n_all ? a.see[t] + 1 : a.n_all;
     }
     const int blocks = (a.n + kKvqBlock - 1) / kKvqBlock;
-    a.per = kKvqWaves;
-    if (blocks <= 2 * kKvqWaves) {
-        a.per = 2 * kKvqWaves;
+    const int tiles = (a.R + 15) / 16, heads = a.c.Hkv;
+    if (blocks <= 8) {
+        a.waves = blocks <= 4 ? 4 : 8;
+        a.per = 8;
+        a.tiles = tiles == 1 || (int64_t)heads * tiles <= n_wg ? 1 : 2;
     } else {
-        int most = n_wg / a.c.Hkv;                       // items per kv head
+        const int fours = (blocks + 3) / 4;
+        a.tiles = tiles == 1 || (int64_t)heads * tiles * fours <= n_wg ? 1 : 2;
+        const int64_t wide = (int64_t)heads * ((tiles + a.tiles - 1) / a.tiles);
+        int most = (int)(n_wg / wide);                     // items per kv head
         most = most < 1 ? 1 : most > kKvqMaxSplits ? kKvqMaxSplits : most;
+        a.waves = fours <= most ? 4 : 8;
         const int least = (blocks + most - 1) / most;
-        if (least > a.per) a.per = (least + kKvqWaves - 1) / kKvqWaves * kKvqWaves;
+        a.per = (least + a.waves - 1) / a.waves * a.waves;
     }
     a.S = (blocks + a.per - 1) / a.per;
     a.mul_S = div_multiplier(a.S);
