@@ -330,18 +330,18 @@ class Model:
     def ad_kvq_read(self, layer: int, pos0: int, n: int):
         """The values of positions pos0 .. pos0 + n - 1 of a layer: (k, v), float32 [n, kv heads, head_dim]."""
         s, torch = self.shape, self.torch
-        k, v = (torch.empty((n, s.n_kv_heads, s.head_dim), dtype=torch.float32, device=self.device) for _ in range(2))
+        k, v = torch.empty((2, n, s.n_kv_heads, s.head_dim), dtype=torch.float32, device=self.device).unbind(0)
         _check(self.L.ad_kvq_read(self.model, self.kv, layer, pos0, n, k.data_ptr(), v.data_ptr(), s.d_kv, _stream_ptr(torch)))
         return k, v
 
     def ad_kvq_attend(self, layer: int, q, pos: Sequence[int]):
         """Attention of rotated queries, float32 [m, query heads, head_dim], row r over positions 0 .. pos[r]: float32 [m, query heads * head_dim]."""
         s, torch = self.shape, self.torch
-        p = np.ascontiguousarray(pos, dtype=np.int32)
+        m = len(pos)
         assert q.dtype == torch.float32 and q.is_contiguous() and q.device == self.device
-        assert q.shape == (p.size, s.n_q_heads, s.head_dim)
-        out = torch.empty((p.size, s.d_q), dtype=torch.float32, device=self.device)
-        _check(self.L.ad_kvq_attend(self.model, self.kv, layer, q.data_ptr(), p.ctypes.data, p.size, out.data_ptr(), _stream_ptr(torch)))
+        assert q.shape == (m, s.n_q_heads, s.head_dim)
+        out = q.new_empty((m, s.d_q))
+        _check(self.L.ad_kvq_attend(self.model, self.kv, layer, q.data_ptr(), (C.c_int32 * m)(*pos), m, out.data_ptr(), _stream_ptr(torch)))
         return out
 
     # ---- steps (device tensors in, device tensors out) ----

@@ -33,19 +33,12 @@ __device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
     return a <= 3.402823466e38f ? a : 0.f;
 }
-// codes of four values already divided by the scale: rounded to nearest even by the conversion (within range by the choice of the scale);
-// the code that is not a number for entries that are not finite
+// codes of four values already divided by the scale: rounded to nearest even by the conversion, within range by the choice of the scale.  Values that are infinite or
+// no numbers become the code that is no number.
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-    auto one = [](float x) { return fabsf(x) <= 448.f ? x : 0.f; };
-    uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(one(a), one(b), 0, false);
-    w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(one(c), one(d), (int)w, true);
-    if (!(fabsf(a) <= 448.f)) w = (w & ~0xffu) | 0x7fu;
-    if (!(fabsf(b) <= 448.f)) w = (w & ~0xff00u) | 0x7f00u;
-    if (!(fabsf(c) <= 448.f)) w = (w & ~0xff0000u) | 0x7f0000u;
-    if (!(fabsf(d) <= 448.f)) w = (w & ~0xff000000u) | 0x7f000000u;
-    return w;
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
-__device__ __forceinline__ uint8_t code1(float x) { return (uint8_t)(codes4(x, 0.f, 0.f, 0.f) & 0xffu); }
 // largest value over N = 8 or 16 neighbouring lanes
 template <int N>
 __device__ __forceinline__ float max_lanes(float v) {
@@ -64,48 +57,80 @@ __device__ __forceinline__ f32x2 values2(uint32_t w) {
 // ---------------------------------------------------------------------------------------------------
 // store and read-out: a workgroup per block of 64 positions and kv head
 // ---------------------------------------------------------------------------------------------------
-// DH / 8 lanes hold a row, 8 entries each, so a wavefront reads 2 KiB of consecutive entries of 4 (8) rows at a time and the largest magnitude
-// is a matter of three (four) moves between lanes.  K rows are stored as they are; V goes through LDS, so that a block of 64 positions that is stored
-// whole leaves in 16-byte pieces.
+// Half of the threads have K, half V.  DH / 8 lanes hold a row, 8 entries each, so that the largest magnitude is a matter of three (four) moves between lanes,
+// and each of them four rows, which are all on their way before the first is looked at.  K rows are stored as they are; V's four codes of a dimension make a
+// word, and go through LDS, so that a block of 64 positions that is stored whole leaves in 16-byte pieces.
+constexpr int kStoreThreads = 512;
 template <int DH>
-__global__ void __launch_bounds__(256) k_kvq_store(KvqRows a) {
-    constexpr int LR = DH / 8, RP = 256 / LR;
-    __shared__ __attribute__((aligned(16))) uint8_t vt[DH][kKvqBlock + 16];
+__global__ void __launch_bounds__(kStoreThreads) k_kvq_store(KvqRows a) {
+    constexpr int LR = DH / 8, T = kStoreThreads / 2, NG = T / LR;         // lanes per row, threads of K, groups of four rows at a time
+    __shared__ uint32_t vt[DH][kKvqBlock / 4 + 1];
     const int tid = threadIdx.x, g = blockIdx.y, p0 = (a.pos0 / kKvqBlock + (int)blockIdx.x) * kKvqBlock;
     const int first = p0 > a.pos0 ? p0 : a.pos0, last = a.pos0 + a.n;
     const int end = p0 + kKvqBlock < last ? p0 + kKvqBlock : last;
+    const bool is_v = tid >= T;
     const int d = tid % LR * 8;
     const KvqCache &c = a.c;
-    for (int p = first + tid / LR; p < end; p += RP) {
-        const size_t at = (size_t)(p - a.pos0) * a.ld + g * DH + d;
+    for (int grp = tid % T / LR; grp < kKvqBlock / 4; grp += NG) {
+        const int pg = p0 + grp * 4;
+        f32x4 x[4][2];
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            const float *src = (kv ? a.v : a.k) + at;
-            const f32x4 x = *(const f32x4 *)src, y = *(const f32x4 *)(src + 4);
+        for (int i = 0; i < 4; ++i) {
+            x[i][0] = x[i][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (pg + i >= first && pg + i < end) {
+                const float *src = (is_v ? a.v : a.k) + (size_t)(pg + i - a.pos0) * a.ld + g * DH + d;
+                x[i][0] = *(const f32x4 *)src;
+                x[i][1] = *(const f32x4 *)(src + 4);
+            }
+        }
+        u32x2 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
             float m = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(finite_abs(x[e]), finite_abs(y[e])));
-            const uint32_t b = scale_byte(max_lanes<LR>(m));
-            const float mul = two_to_minus(b);
-            const u32x2 w = {codes4(x[0] * mul, x[1] * mul, x[2] * mul, x[3] * mul), codes4(y[0] * mul, y[1] * mul, y[2] * mul, y[3] * mul)};
-            if (d == 0) (kv ? c.Vs : c.Ks)[(size_t)g * c.stride + p] = (uint8_t)b;
-            if (kv == 0) {
-                *(u32x2 *)(c.Kc + ((size_t)g * c.stride + p) * DH + d) = w;
-            } else {
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(x[i][0][e]), fabsf(x[i][1][e])));
+            m = max_lanes<LR>(m);
+            if (m == INFINITY) {                           // (the same in all lanes of a row)
+                m = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) vt[d + e][p - p0] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(finite_abs(x[i][0][e]), finite_abs(x[i][1][e])));
+                m = max_lanes<LR>(m);
+            }
+            const uint32_t b = scale_byte(m);
+            const float mul = two_to_minus(b);
+            w[i] = (u32x2){codes4(x[i][0][0] * mul, x[i][0][1] * mul, x[i][0][2] * mul, x[i][0][3] * mul),
+                           codes4(x[i][1][0] * mul, x[i][1][1] * mul, x[i][1][2] * mul, x[i][1][3] * mul)};
+            if (pg + i >= first && pg + i < end) {
+                const size_t row = (size_t)g * c.stride + pg + i;
+                if (d == 0) (is_v ? c.Vs : c.Ks)[row] = (uint8_t)b;
+                if (!is_v) *(u32x2 *)(c.Kc + row * DH + d) = w[i];
+            }
+        }
+        if (is_v) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // 4 x 4 bytes turned over: [position][dimension] -> [dimension][position]
+                const uint32_t lo01 = __builtin_amdgcn_perm(w[1][h], w[0][h], 0x05010400u), hi01 = __builtin_amdgcn_perm(w[1][h], w[0][h], 0x07030602u);
+                const uint32_t lo23 = __builtin_amdgcn_perm(w[3][h], w[2][h], 0x05010400u), hi23 = __builtin_amdgcn_perm(w[3][h], w[2][h], 0x07030602u);
+                vt[d + 4 * h][grp] = (lo01 & 0xffffu) | lo23 << 16;
+                vt[d + 4 * h + 1][grp] = lo01 >> 16 | (lo23 & 0xffff0000u);
+                vt[d + 4 * h + 2][grp] = (hi01 & 0xffffu) | hi23 << 16;
+                vt[d + 4 * h + 3][grp] = hi01 >> 16 | (hi23 & 0xffff0000u);
             }
         }
     }
     __syncthreads();
     uint8_t *V = c.Vc + ((size_t)g * c.stride + p0) * DH;
     if (first == p0 && end == p0 + kKvqBlock) {
-        for (int i = tid; i < DH * 4; i += 256) *(u32x4 *)(V + i * 16) = *(const u32x4 *)&vt[i >> 2][(i & 3) * 16];
+        for (int i = tid; i < DH * 4; i += kStoreThreads) {
+            const uint32_t *src = &vt[i >> 2][(i & 3) * 4];
+            *(u32x4 *)(V + i * 16) = (u32x4){src[0], src[1], src[2], src[3]};
+        }
     } else {
         const int n = end - first;
-        for (int i = tid; i < DH * n; i += 256) {
+        for (int i = tid; i < DH * n; i += kStoreThreads) {
             const int e = i / n, p = first - p0 + i % n;
-            V[e * kKvqBlock + p] = vt[e][p];
+            V[e * kKvqBlock + p] = (uint8_t)(vt[e][p >> 2] >> (8 * (p & 3)));
         }
     }
 }
@@ -167,7 +192,8 @@ __global__ void __launch_bounds__(256) k_kvq_rotate(KvqRotate a) {
     const int g = head - a.Hq - (is_v ? a.c.Hkv : 0), p = a.pos0 + t;
     const uint32_t b = scale_byte(max64(fmaxf(finite_abs(x), finite_abs(y))));
     const float mul = two_to_minus(b);
-    const uint8_t c0 = code1(x * mul), c1 = code1(y * mul);
+    const uint32_t cc = codes4(x * mul, y * mul, 0.f, 0.f);
+    const uint8_t c0 = (uint8_t)cc, c1 = (uint8_t)(cc >> 8);
     if (!live) return;
     const size_t at = (size_t)g * a.c.stride + p;
     if (is_v) {
@@ -306,6 +332,7 @@ template <int DH, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW, NW / 4) k_kvq_attn(KvqAttn a) {
     constexpr int J = DH / 64, DT = DH / 16, RP = RT * 16, PR = DH + 2, NTH = 64 * NW, KU = KvqAttnLds<DH, RT, NW>::KU;
     constexpr int NK = 4 * J + 1, NV = DT;                 // copies of a block's K (with the scales), of its V
+    warm_kernel_args<sizeof(KvqAttn)>();
     constexpr int kPBits = 14;                             // probabilities times 2^14: those of 2^-17 and more keep 21 bits in fp16 hi and lo
     extern __shared__ __attribute__((aligned(16))) char lds_raw[];
     KvqAttnLds<DH, RT, NW> &L = *reinterpret_cast<KvqAttnLds<DH, RT, NW> *>(lds_raw);
@@ -712,8 +739,8 @@ dim3 rows_grid(const KvqRows &a) { return dim3((a.pos0 + a.n - 1) / kKvqBlock - 
 
 int launch_kvq_store(const KvqRows &a, const LaunchCtx &c) {
     if (!rows_ok(a)) return (int)hipErrorInvalidValue;
-    if (a.c.dh == 128) return launch<k_kvq_store<128>>(c, rows_grid(a), dim3(256), 0, a);
-    if (a.c.dh == 64) return launch<k_kvq_store<64>>(c, rows_grid(a), dim3(256), 0, a);
+    if (a.c.dh == 128) return launch<k_kvq_store<128>>(c, rows_grid(a), dim3(kStoreThreads), 0, a);
+    if (a.c.dh == 64) return launch<k_kvq_store<64>>(c, rows_grid(a), dim3(kStoreThreads), 0, a);
     return (int)hipErrorInvalidValue;
 }
 
