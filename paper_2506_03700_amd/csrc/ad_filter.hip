@@ -12,6 +12,7 @@
 //                     buckets that the boundaries lie in
 //   k_filter_row      weight of each segment's ids that are kept for certain, and a list of the ids in the boundaries' buckets; the
 //                     last workgroup of the row finds the boundaries among those, and draws
+//   k_filter_one      all of that for a row of one segment
 //   k_filter_probs, k_filter_verify: from the rows' outcomes
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -27,7 +28,10 @@ namespace ad {
 namespace {
 
 constexpr int NT = kFilterThreads, NW = NT / 64;
-constexpr int kRank = NT;                                // entries that are ranked against each other
+constexpr int kRank = 64;                                // entries that are ranked against each other
+constexpr int kKeep = kFilterSegIds / NT;                // logits that a thread keeps (longer segments read the others again)
+constexpr int kEntries = 2048;                           // entries of a list that are taken into LDS
+constexpr int kLinear = 1792;                            // buckets of equal width
 
 // ---------------------------------------------------------------------------------------------------
 // keys, weights, buckets
@@ -49,7 +53,6 @@ __device__ __forceinline__ uint64_t whole(double w, int bits) { return (uint64_t
 // 28 times the temperature below the top in steps of 1/64, then 16 steps for each factor of two
 __device__ __forceinline__ int bucket_of(float z, float top, float scale) {
     const float x = (top - z) * scale;
-    constexpr int kLinear = 1792;
     if (x < (float)kLinear) return (int)x;
     const uint32_t b = (__float_as_uint(x) - __float_as_uint((float)kLinear)) >> 19;
     return kLinear + (int)(b < kFilterBuckets - 1 - kLinear ? b : kFilterBuckets - 1 - kLinear);
@@ -79,13 +82,24 @@ __device__ __forceinline__ float block_top(float v, BlockLds &L) {
     for (int w = 1; w < NW; ++w) r = (r != r || L.f[w] != L.f[w]) ? __uint_as_float(0x7fc00000u) : fmaxf(r, L.f[w]);
     return r;
 }
+// v of the lane that DPP control CTRL names, 0 where there is none
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_u64(uint64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xf, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xf, 0xf, false);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v, int lane) {     // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
+    v += dpp_u64<0x111>(v);                              // row_shr 1, 2, 4, 8: within a row of 16 lanes
+    v += dpp_u64<0x112>(v);
+    v += dpp_u64<0x114>(v);
+    v += dpp_u64<0x118>(v);
+    const uint64_t r0 = lane_u64(v, 15), r1 = r0 + lane_u64(v, 31), r2 = r1 + lane_u64(v, 47);
+    const int row = lane >> 4;
+    return v + (row == 0 ? 0 : row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 // sum over the threads before this one; *total: over all
 __device__ __forceinline__ uint64_t block_scan(uint64_t v, BlockLds &L, uint64_t *total) {
@@ -135,22 +149,48 @@ __device__ __forceinline__ bool last_of(uint32_t *counter, int n, BlockLds &L) {
     return last_to_arrive(counter, n, &L.last_wg);
 }
 
+// A segment's logits: a thread has ids j0 + tid, + NT, ...; the first kKeep of them, all on their way at once, stay in registers.
+struct SegLogits {
+    const float *z;
+    int j0, j1;
+    float v[kKeep];
+    __device__ __forceinline__ void load(const FilterArgs &a, int r, int seg) {
+        z = row_of(a, r);
+        j0 = seg * a.seg_ids;
+        j1 = min(a.V, j0 + a.seg_ids);
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            const int j = j0 + (int)threadIdx.x + i * NT;
+            v[i] = j < j1 ? z[j] : -INFINITY;
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) f(v[i], j0 + (int)threadIdx.x + i * NT);        // (past the end: minus infinity)
+        for (int j = j0 + (int)threadIdx.x + kKeep * NT; j < j1; j += NT) f(z[j], j);
+    }
+    // largest logit, not a number if one is none
+    __device__ __forceinline__ float top(BlockLds &L) const {
+        float m = -INFINITY;
+        bool nan = false;
+        each([&](float x, int) {
+            nan |= x != x;
+            m = fmaxf(m, x);
+        });
+        return block_top(nan ? __uint_as_float(0x7fc00000u) : m, L);
+    }
+};
+
 // ---------------------------------------------------------------------------------------------------
 // 1. largest logits
 // ---------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(NT) k_filter_top(FilterArgs a) {
     __shared__ BlockLds L;
-    const int r = blockIdx.y, j0 = blockIdx.x * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids);
-    const float *z = row_of(a, r);
-    float m = -INFINITY;
-    bool nan = false;
-    for (int j = j0 + (int)threadIdx.x; j < j1; j += NT) {
-        const float x = z[j];
-        nan |= x != x;
-        m = fmaxf(m, x);
-    }
-    m = block_top(nan ? __uint_as_float(0x7fc00000u) : m, L);
-    if (threadIdx.x == 0) a.s->seg_top[r][blockIdx.x] = m;
+    SegLogits z;
+    z.load(a, blockIdx.y, blockIdx.x);
+    const float m = z.top(L);
+    if (threadIdx.x == 0) a.s->seg_top[blockIdx.y][blockIdx.x] = m;
 }
 
 // of the row, to every thread; *bad: it has no distribution
@@ -163,70 +203,50 @@ __device__ __forceinline__ float row_top(const FilterArgs &a, int r, BlockLds &L
 // ---------------------------------------------------------------------------------------------------
 // 2. buckets
 // ---------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
-    __shared__ BlockLds L;
-    __shared__ uint64_t hw[kFilterBuckets];
-    __shared__ uint32_t hc[kFilterBuckets];
-    const int r = blockIdx.y, tid = threadIdx.x, j0 = blockIdx.x * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids);
-    const float *z = row_of(a, r);
-    FilterScratch &S = *a.s;
-    bool bad;
-    const float top = row_top(a, r, L, &bad);
-    for (int b = tid; b < kFilterBuckets; b += NT) {
-        hw[b] = 0;
-        hc[b] = 0;
-    }
-    __syncthreads();
-    if (!bad) {
-        for (int j = j0 + tid; j < j1; j += NT) {
-            const float x = z[j];
-            if (masked(x)) continue;
-            const int b = bucket_of(x, top, a.bucket_scale);
-            atomicAdd(&hc[b], 1u);
-            atomicAdd((unsigned long long *)&hw[b], (unsigned long long)whole(weight_of(x, top, a.inv_t), a.weight_bits));
+// Weights are needed for top-p, counts for top-k: the other array is left alone.
+struct Histogram {
+    uint64_t weight[kFilterBuckets];
+    uint32_t count[kFilterBuckets];
+    __device__ __forceinline__ void clear(const FilterArgs &a) {
+        for (int b = threadIdx.x; b < kFilterBuckets; b += NT) {
+            if (a.top_p < 1.0) weight[b] = 0;
+            if (a.top_k) count[b] = 0;
         }
     }
-    __syncthreads();
-    for (int b = tid; b < kFilterBuckets; b += NT)
-        if (hc[b]) {
-            atomicAdd(&S.count[r][b], hc[b]);
-            atomicAdd((unsigned long long *)&S.weight[r][b], (unsigned long long)hw[b]);
-        }
-    if (!last_of(S.arrivals[r], a.n_seg, L)) return;
+    __device__ __forceinline__ void add(const FilterArgs &a, float x, float top) {
+        if (masked(x)) return;
+        const int b = bucket_of(x, top, a.bucket_scale);
+        if (a.top_k) atomicAdd(&count[b], 1u);
+        if (a.top_p < 1.0) atomicAdd((unsigned long long *)&weight[b], (unsigned long long)whole(weight_of(x, top, a.inv_t), a.weight_bits));
+    }
+};
 
-    // the last workgroup: thread t has buckets 4 t .. 4 t + 3
+// The buckets of the boundaries from those of the whole row, of which thread t has 4 t .. 4 t + 3 (w and c are zero where that step is off).  By one workgroup.
+__device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t (&w)[kFilterBuckets / NT], const uint32_t (&c)[kFilterBuckets / NT],
+                                             FilterRow &R, BlockLds &L) {
     constexpr int PER = kFilterBuckets / NT;
-    uint64_t w[PER], c[PER], ws = 0, cs = 0;
+    const int tid = threadIdx.x;
+    __shared__ uint64_t in_k;
+    uint64_t ws = 0, cs = 0, w0 = 0, c0 = 0, all_w = 0, all_c = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        w[i] = seen(&S.weight[r][tid * PER + i]);
-        c[i] = seen(&S.count[r][tid * PER + i]);
         ws += w[i];
         cs += c[i];
     }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {                      // zero for the next call
-        leave(&S.weight[r][tid * PER + i], (uint64_t)0);
-        leave(&S.count[r][tid * PER + i], 0u);
-    }
-    uint64_t all_w, all_c;
-    const uint64_t w0 = block_scan(ws, L, &all_w), c0 = block_scan(cs, L, &all_c);
-    __shared__ FilterRow R;
     if (tid == 0) {
         R.p0 = kFilterBuckets;
         R.p1 = -1;
         R.bk = -1;
         R.count_k = 0;
         R.weight_p = R.weight_k = 0;
-        R.weight = all_w;
+        in_k = 0;
     }
-    __syncthreads();
+    if (a.top_p < 1.0) w0 = block_scan(ws, L, &all_w);
+    if (a.top_k) c0 = block_scan(cs, L, &all_c);
+    if (tid == 0) R.weight = all_w;
     // top-k: the bucket of the last id it keeps (none if it keeps them all)
-    uint64_t cb = c0, wb = w0;
-    __shared__ uint64_t in_k;
-    if (tid == 0) in_k = 0;
-    __syncthreads();
     if (a.top_k && (uint64_t)a.top_k < all_c) {
+        uint64_t cb = c0, wb = w0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (cb < (uint64_t)a.top_k && cb + c[i] >= (uint64_t)a.top_k) {
@@ -240,29 +260,59 @@ __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
         }
     }
     __syncthreads();
-    // top-p: its share of what top-k keeps, which is known up to that bucket's weight; the buckets that it may end in
     if (a.top_p < 1.0) {
-        const double lo = a.top_p * (double)(R.bk >= 0 ? R.weight_k : all_w), hi = a.top_p * (double)(R.bk >= 0 ? R.weight_k + in_k : all_w);
-        wb = w0;
+        // top-p: its share of what top-k keeps, which is known up to that bucket's weight; the buckets that it may end in
+        // (a factor for the roundings of these sums to doubles: more buckets than need be do no harm)
+        const double lo = a.top_p * (double)(R.bk >= 0 ? R.weight_k : all_w) * (1.0 - 1e-12);
+        const double hi = a.top_p * (double)(R.bk >= 0 ? R.weight_k + in_k : all_w) * (1.0 + 1e-12);
+        uint64_t wb = w0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            // (a factor for the roundings of these sums to doubles: more buckets than need be do no harm)
-            const bool before = (double)(wb + w[i]) < lo * (1.0 - 1e-12), behind = (double)wb > hi * (1.0 + 1e-12);
-            if (c[i] && !before && !behind) {
-                atomicMin(&R.p0, tid * PER + i);
-                atomicMax(&R.p1, tid * PER + i);
+            // the first bucket that reaches lo, the last that starts at or before hi (the buckets in between may be empty)
+            const bool before = (double)(wb + w[i]) < lo, behind = (double)wb > hi;
+            if (!before && ((double)wb < lo || tid * PER + i == 0)) {
+                R.p0 = tid * PER + i;
+                R.weight_p = wb;
             }
-            wb += w[i];
-        }
-        __syncthreads();
-        wb = w0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (R.p0 == tid * PER + i) R.weight_p = wb;
+            if (!behind && (double)(wb + w[i]) > hi) R.p1 = tid * PER + i;
             wb += w[i];
         }
     }
     __syncthreads();
+}
+
+__global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
+    __shared__ BlockLds L;
+    __shared__ Histogram H;
+    __shared__ FilterRow R;
+    const int r = blockIdx.y, tid = threadIdx.x;
+    FilterScratch &S = *a.s;
+    SegLogits z;
+    z.load(a, r, blockIdx.x);
+    H.clear(a);
+    bool bad;
+    const float top = row_top(a, r, L, &bad);
+    if (!bad) z.each([&](float x, int) { H.add(a, x, top); });
+    __syncthreads();
+    for (int b = tid; b < kFilterBuckets; b += NT) {
+        if (a.top_k && H.count[b]) atomicAdd(&S.count[r][b], H.count[b]);
+        if (a.top_p < 1.0 && H.weight[b]) atomicAdd((unsigned long long *)&S.weight[r][b], (unsigned long long)H.weight[b]);
+    }
+    if (!last_of(S.arrivals[r], a.n_seg, L)) return;
+    constexpr int PER = kFilterBuckets / NT;
+    uint64_t w[PER];
+    uint32_t c[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        w[i] = a.top_p < 1.0 ? seen(&S.weight[r][tid * PER + i]) : 0;
+        c[i] = a.top_k ? seen(&S.count[r][tid * PER + i]) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {                      // zero for the next call
+        if (a.top_p < 1.0) leave(&S.weight[r][tid * PER + i], (uint64_t)0);
+        if (a.top_k) leave(&S.count[r][tid * PER + i], 0u);
+    }
+    find_buckets(a, w, c, R, L);
     if (tid == 0) S.row[r] = R;
 }
 
@@ -295,11 +345,11 @@ struct Entries {
 };
 
 struct SelectLds {
-    uint64_t m[NT];                                      // measure by bin; then of the entries that are ranked
-    uint64_t key[kRank];
-    uint32_t c[NT];
-    int n, bin;
-    uint64_t before;
+    uint64_t m[NT];                                      // measure, or weight, by bin
+    uint32_t c[NT];                                      // entries by bin
+    uint64_t key[kRank], w[kRank];                       // the entries that are ranked
+    int n, bin, bin_n;
+    uint64_t before, before_w;
 };
 
 // The ids of buckets b0 .. b1 in their order; an id is kept if the measures (1 each, or the weights) of the ones before it add up to less than `limit`.
@@ -368,17 +418,96 @@ __device__ uint64_t least_kept(const Entries &E, int b0, int b1, uint64_t limit,
         if (k < lo || k > hi) continue;
         const int at = atomicAdd(&S.n, 1);
         S.key[at] = k;
-        S.m[at] = measure(x);
+        S.w[at] = measure(x);
     }
     __syncthreads();
     uint64_t least = hi + 1;
     if (tid < S.n) {
         const uint64_t mine = S.key[tid];
         uint64_t before = 0;
-        for (int i = 0; i < S.n; ++i) before += S.key[i] > mine ? S.m[i] : 0;
+        for (int i = 0; i < S.n; ++i) before += S.key[i] > mine ? S.w[i] : 0;
         if (before < limit) least = mine;
     }
     return block_extreme<false>(least, L);
+}
+
+// A list in LDS: keys, weights and buckets of its entries.
+struct EntryLds {
+    uint64_t key[kEntries], w[kEntries];
+    uint16_t bucket[kEntries];
+    __device__ __forceinline__ void put(const FilterArgs &a, int at, float x, int id, float top) {
+        key[at] = key_of(x, id);
+        w[at] = whole(weight_of(x, top, a.inv_t), a.weight_bits);
+        bucket[at] = (uint16_t)bucket_of(x, top, a.bucket_scale);
+    }
+};
+__device__ __forceinline__ float logit_of(uint64_t key) {
+    const uint32_t u = (uint32_t)(key >> 32);
+    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+__device__ __forceinline__ int id_of(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+
+// least_kept for the common case, a list in LDS: the buckets of equal width cut once more into NT bins, and no more than kRank entries in the boundary's bin, which
+// every wavefront ranks for itself.  False if it is not that case.  *weight: of what is kept (for counts; the weights are measured too).
+template <bool WEIGHTS>
+__device__ __forceinline__ bool least_kept_lds(const FilterArgs &a, const EntryLds &T, int n, int b0, int b1, uint64_t limit, float top, SelectLds &S, BlockLds &L,
+                                               uint64_t *least, uint64_t *weight) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (b1 >= kLinear || limit == 0) return false;
+    const float fine = (float)NT / (float)(b1 - b0 + 1);
+    auto bin_of = [&](int i) {                           // (monotonic in the logit)
+        float x = (top - logit_of(T.key[i])) * a.bucket_scale;
+        asm("" : "+v"(x));                               // (the same rounding both times)
+        const int b = (int)((x - (float)b0) * fine);
+        return b < 0 ? 0 : b < NT ? b : NT - 1;
+    };
+    __syncthreads();
+    S.m[tid] = 0;
+    S.c[tid] = 0;
+    if (tid == 0) S.n = S.bin = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) {
+        if (T.bucket[i] < b0 || T.bucket[i] > b1) continue;
+        const int b = bin_of(i);
+        atomicAdd(&S.c[b], 1u);
+        atomicAdd((unsigned long long *)&S.m[b], (unsigned long long)T.w[i]);
+    }
+    __syncthreads();
+    uint64_t all, before_c = 0;
+    const uint64_t before_w = block_scan(S.m[tid], L, &all);
+    if (!WEIGHTS) before_c = block_scan(S.c[tid], L, &all);
+    const uint64_t before = WEIGHTS ? before_w : before_c;
+    if (S.c[tid] && before < limit) atomicMax(&S.bin, tid);
+    __syncthreads();
+    const int bin = S.bin;
+    if (tid == bin) {
+        S.before = before;
+        S.before_w = before_w;
+        S.bin_n = (int)S.c[tid];
+    }
+    __syncthreads();
+    const int nb = S.bin_n;
+    if (nb > kRank || nb == 0) return false;
+    for (int i = tid; i < n; i += NT) {
+        if (T.bucket[i] < b0 || T.bucket[i] > b1 || bin_of(i) != bin) continue;
+        const int at = atomicAdd(&S.n, 1);
+        S.key[at] = T.key[i];
+        S.w[at] = T.w[i];
+    }
+    __syncthreads();
+    const uint64_t mine = lane < nb ? S.key[lane] : 0, left = limit - S.before;
+    uint64_t ahead = 0;
+    int rank = 0;
+    for (int i = 0; i < nb; ++i) {
+        const bool greater = S.key[i] > mine;
+        rank += greater;
+        ahead += greater ? (WEIGHTS ? S.w[i] : 1) : 0;
+    }
+    const bool kept = lane < nb && ahead < left;
+    const int n_kept = __popcll(__ballot(kept));         // one at least: nothing is ahead of the first
+    *least = lane_u64(mine, __ffsll(__ballot(lane < nb && rank == n_kept - 1)) - 1);
+    *weight = S.before_w + lane_u64(wave_scan(kept ? S.w[lane] : 0, lane), 63);
+    return true;
 }
 
 // what the outcome of a row says about an id
@@ -440,19 +569,86 @@ __device__ __forceinline__ void report_draw(const FilterArgs &a, int tok, float 
     report_done(a.done_flag, a.done_seq);
 }
 
+// The smallest key that top-k and top-p keep, R saying which buckets their boundaries lie in.  n: entries in T, negative if they are not there.
+__device__ __forceinline__ uint64_t find_least(const FilterArgs &a, const FilterRow &R, const Entries &E, const EntryLds &T, int n, float top, SelectLds &S, BlockLds &L) {
+    uint64_t least = 0, weight = R.weight;
+    if (R.bk >= 0) {
+        const uint64_t limit = (uint64_t)a.top_k - R.count_k;
+        uint64_t in_bucket;
+        if (n < 0 || !least_kept_lds<false>(a, T, n, R.bk, R.bk, limit, top, S, L, &least, &in_bucket)) {
+            least = least_kept<false>(E, R.bk, R.bk, limit, S, L);
+            in_bucket = 0;
+            for (int i = threadIdx.x; i < E.count(); i += NT) {
+                float x;
+                int id;
+                if (E.get(i, R.bk, R.bk, x, id) && key_of(x, id) >= least) in_bucket += whole(weight_of(x, top, a.inv_t), a.weight_bits);
+            }
+            in_bucket = block_sum(in_bucket, L);
+        }
+        weight = R.weight_k + in_bucket;
+    }
+    if (R.p0 <= R.p1) {
+        // kept: less than top_p * weight before it
+        const uint64_t bound = (uint64_t)ceil(a.top_p * (double)weight), limit = bound > R.weight_p ? bound - R.weight_p : 0;
+        uint64_t by_p, ignore;
+        if (n < 0 || !least_kept_lds<true>(a, T, n, R.p0, R.p1, limit, top, S, L, &by_p, &ignore)) by_p = least_kept<true>(E, R.p0, R.p1, limit, S, L);
+        least = by_p > least ? by_p : least;
+    }
+    return least;
+}
+
+// buckets before `sure` are kept as far as top-k and top-p go, those of the boundaries are listed
+struct Classes {
+    int sure, p0, p1, bk;
+    __device__ __forceinline__ Classes(const FilterRow &R) : sure(R.p0 <= R.p1 ? R.p0 : R.bk >= 0 ? R.bk : kFilterBuckets), p0(R.p0), p1(R.p1), bk(R.bk) {}
+    __device__ __forceinline__ bool listed(int b) const { return b == bk || (b >= p0 && b <= p1); }
+};
+
+__device__ __forceinline__ void no_distribution(const FilterArgs &a, int r, float top) {
+    if (threadIdx.x != 0) return;
+    FilterRow &R = a.s->row[r];
+    R.bad = 1;
+    R.top = top;
+    R.least = ~0ull;
+    R.total = 0;
+    if (a.tok_out) report_draw(a, -1, __uint_as_float(0x7fc00000u));
+}
+
+// The row's outcome for the kernels that follow; thread t has the weight of segment t.  Returns the weight of all.
+__device__ __forceinline__ uint64_t outcome(const FilterArgs &a, int r, float top, uint64_t least, uint64_t w, BlockLds &L) {
+    uint64_t total;
+    (void)block_scan(w, L, &total);
+    if ((int)threadIdx.x < a.n_seg) a.s->seg_weight[r][threadIdx.x] = w;
+    if (threadIdx.x == 0) {
+        FilterRow &R = a.s->row[r];
+        R.bad = 0;
+        R.top = top;
+        R.least = least;
+        R.total = total;
+    }
+    return total;
+}
+
+__device__ __forceinline__ void draw_and_report(const FilterArgs &a, const Kept &kept, const float *z, uint64_t w, WalkLds &K, BlockLds &L) {
+    double x;
+    uint64_t total;
+    const int tok = draw(a, w, a.u, [&](int j) { return kept(z[j], j); }, K, L, &x, &total);
+    if (threadIdx.x == 0) report_draw(a, tok, (float)(x / ldexp((double)total, -a.weight_bits)));
+}
+
 // BOUND: there are boundaries to find (k_filter_buckets has run)
 template <bool BOUND>
 __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     __shared__ BlockLds L;
     __shared__ SelectLds SL;
+    __shared__ EntryLds T;
     __shared__ WalkLds K;
     __shared__ uint64_t seg_w[kFilterMaxSegs];
     __shared__ int n_mine, at_mine;
-    const int r = blockIdx.y, tid = threadIdx.x, j0 = blockIdx.x * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids);
-    const float *z = row_of(a, r);
+    const int r = blockIdx.y, tid = threadIdx.x;
     FilterScratch &S = *a.s;
-    bool bad;
-    const float top = row_top(a, r, L, &bad);
+    SegLogits z;
+    z.load(a, r, blockIdx.x);
     FilterRow R;
     if constexpr (BOUND) {
         R = S.row[r];
@@ -460,32 +656,47 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
         R.p0 = kFilterBuckets;
         R.p1 = R.bk = -1;
     }
-    // buckets before `sure` are kept, those of the boundaries are listed
-    const int sure = R.p0 <= R.p1 ? R.p0 : R.bk >= 0 ? R.bk : kFilterBuckets;
+    const Classes in(R);
+    if (tid == 0) n_mine = 0;
+    bool bad;
+    const float top = row_top(a, r, L, &bad);            // (a barrier or two)
     uint64_t mine = 0;
     if (!bad) {
-        for (int base = j0; base < j1; base += NT) {
-            const int j = base + tid;
-            const float x = j < j1 ? z[j] : -INFINITY;
-            bool listed = false;
-            if (!masked(x)) {
-                const int b = BOUND ? bucket_of(x, top, a.bucket_scale) : 0;
-                if (b < sure) {
-                    const double w = weight_of(x, top, a.inv_t);
-                    if (w >= a.min_p) mine += whole(w, a.weight_bits);
-                } else {
-                    listed = b == R.bk || (b >= R.p0 && b <= R.p1);
-                }
+        auto sure = [&](float x) {
+            const double w = weight_of(x, top, a.inv_t);
+            if (w >= a.min_p) mine += whole(w, a.weight_bits);
+        };
+        if constexpr (!BOUND) {
+            z.each([&](float x, int) {
+                if (!masked(x)) sure(x);
+            });
+        } else {
+            auto put = [&](uint32_t at, float x, int j) {
+                if (at < kFilterList) leave(&S.list[r][at], (uint64_t)__float_as_uint(x) << 32 | (uint32_t)j);
+            };
+            unsigned listed = 0;                          // of the kept logits, by their place
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) {
+                if (masked(z.v[i])) continue;
+                const int b = bucket_of(z.v[i], top, a.bucket_scale);
+                if (b < in.sure) sure(z.v[i]);
+                else listed |= in.listed(b) ? 1u << i : 0;
             }
-            if constexpr (BOUND) {
-                if (tid == 0) n_mine = 0;
-                __syncthreads();
-                int at = 0;
-                if (listed) at = atomicAdd(&n_mine, 1);
-                __syncthreads();
-                if (tid == 0 && n_mine) at_mine = (int)atomicAdd(&S.list_n[r][0], (uint32_t)n_mine);
-                __syncthreads();
-                if (listed && at_mine + at < kFilterList) leave(&S.list[r][at_mine + at], (uint64_t)__float_as_uint(x) << 32 | (uint32_t)j);
+            const int n = __popc(listed);
+            int at = n ? atomicAdd(&n_mine, n) : 0;
+            __syncthreads();
+            if (tid == 0 && n_mine) at_mine = (int)atomicAdd(&S.list_n[r][0], (uint32_t)n_mine);
+            __syncthreads();
+            at += at_mine;
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if (listed >> i & 1) put((uint32_t)at++, z.v[i], z.j0 + tid + i * NT);
+            for (int j = z.j0 + tid + kKeep * NT; j < z.j1; j += NT) {           // (segments beyond the usual length)
+                const float x = z.z[j];
+                if (masked(x)) continue;
+                const int b = bucket_of(x, top, a.bucket_scale);
+                if (b < in.sure) sure(x);
+                else if (in.listed(b)) put(atomicAdd(&S.list_n[r][0], 1u), x, j);
             }
         }
     }
@@ -494,71 +705,117 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     if (!last_of(S.arrivals[r], a.n_seg, L)) return;
 
     if (bad) {
-        if (tid == 0) {
-            S.row[r].bad = 1;
-            S.row[r].top = top;
-            S.row[r].least = ~0ull;
-            S.row[r].total = 0;
-            if (a.tok_out) report_draw(a, -1, __uint_as_float(0x7fc00000u));
-        }
+        no_distribution(a, r, top);
         return;
     }
-    uint64_t w = tid < a.n_seg ? seen(&S.seg_weight[r][tid]) : 0, least = 0;
+    uint64_t w = tid < a.n_seg ? seen(&S.seg_weight[r][tid]) : 0;
     Kept kept{0, top, a.inv_t, a.min_p};
     if constexpr (BOUND) {
-        const uint32_t n = seen(&S.list_n[r][0]);
-        const Entries E{z, S.list[r], n <= kFilterList ? (int)n : -1, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
-        uint64_t weight = R.weight;
-        if (R.bk >= 0) {
-            least = least_kept<false>(E, R.bk, R.bk, (uint64_t)a.top_k - R.count_k, SL, L);
-            weight = 0;
-            for (int i = tid; i < E.count(); i += NT) {
-                float x;
-                int id;
-                if (E.get(i, R.bk, R.bk, x, id) && key_of(x, id) >= least) weight += whole(weight_of(x, top, a.inv_t), a.weight_bits);
-            }
-            weight = R.weight_k + block_sum(weight, L);
+        const uint32_t n_all = seen(&S.list_n[r][0]);
+        const int n = n_all <= kEntries ? (int)n_all : -1;
+        const Entries E{z.z, S.list[r], n_all <= kFilterList ? (int)n_all : -1, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
+        for (int i = tid; i < n; i += NT) {
+            const uint64_t e = seen(&S.list[r][i]);
+            T.put(a, i, __uint_as_float((uint32_t)(e >> 32)), (int)(uint32_t)e, top);
         }
-        if (R.p0 <= R.p1) {
-            // kept: less than top_p * weight before it
-            const uint64_t bound = (uint64_t)ceil(a.top_p * (double)weight);
-            const uint64_t by_p = least_kept<true>(E, R.p0, R.p1, bound > R.weight_p ? bound - R.weight_p : 0, SL, L);
-            least = by_p > least ? by_p : least;
-        }
-        kept.least = least;
+        kept.least = find_least(a, R, E, T, n, top, SL, L);
         // the listed ones that are kept join their segments
-        __syncthreads();
         seg_w[tid] = w;
         __syncthreads();
         auto join = [&](float x, int id) {
             const uint64_t y = whole(kept(x, id), a.weight_bits);
             if (y) atomicAdd((unsigned long long *)&seg_w[id / a.seg_ids], (unsigned long long)y);
         };
-        for (int i = tid; i < E.count(); i += NT) {
-            float x;
-            int id;
-            const bool in_p = E.get(i, R.p0, R.p1, x, id);
-            if (in_p || E.get(i, R.bk, R.bk, x, id)) join(x, id);
+        if (n >= 0) {
+            for (int i = tid; i < n; i += NT)
+                if (T.key[i] >= kept.least) join(logit_of(T.key[i]), id_of(T.key[i]));
+        } else {
+            for (int i = tid; i < E.count(); i += NT) {
+                float x;
+                int id;
+                const bool in_p = E.get(i, R.p0, R.p1, x, id);
+                if (in_p || E.get(i, R.bk, R.bk, x, id)) join(x, id);
+            }
         }
         __syncthreads();
         w = seg_w[tid];
         if (tid == 0) leave(&S.list_n[r][0], 0u);
     }
-    if (a.tok_out) {
-        double x;
-        uint64_t total;
-        const int tok = draw(a, w, a.u, [&](int j) { return kept(z[j], j); }, K, L, &x, &total);
-        if (tid == 0) report_draw(a, tok, (float)(x / ldexp((double)total, -a.weight_bits)));
+    if (a.tok_out) draw_and_report(a, kept, z.z, w, K, L);
+    else (void)outcome(a, r, top, kept.least, w, L);
+}
+
+// A row of one segment: everything, with what the kernels above leave one another in LDS.  It writes the distribution if that is asked for.
+__global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
+    __shared__ BlockLds L;
+    __shared__ SelectLds SL;
+    __shared__ union { Histogram H; EntryLds T; } M;
+    __shared__ WalkLds K;
+    __shared__ FilterRow R;
+    __shared__ int n_listed;
+    const int r = blockIdx.x, tid = threadIdx.x;
+    SegLogits z;
+    z.load(a, r, 0);
+    const float top = z.top(L);
+    if (!(fabsf(top) < INFINITY)) {
+        no_distribution(a, r, top);
+        if (probs) z.each([&](float, int j) {
+            if (j < a.V) probs[(size_t)r * a.V + j] = __uint_as_float(0x7fc00000u);
+        });
         return;
     }
-    uint64_t total;
-    (void)block_scan(w, L, &total);
-    if (tid < a.n_seg) S.seg_weight[r][tid] = w;
-    if (tid == 0) {
-        S.row[r].bad = 0;
-        S.row[r].top = top;
-        S.row[r].least = least;
-        S.row[r].total = total;
+    Kept kept{0, top, a.inv_t, a.min_p};
+    uint64_t mine = 0;
+    if (a.top_k || a.top_p < 1.0) {
+        M.H.clear(a);
+        if (tid == 0) n_listed = 0;
+        __syncthreads();
+        z.each([&](float x, int) { M.H.add(a, x, top); });
+        __syncthreads();
+        constexpr int PER = kFilterBuckets / NT;
+        uint64_t w[PER];
+        uint32_t c[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            w[i] = a.top_p < 1.0 ? M.H.weight[tid * PER + i] : 0;
+            c[i] = a.top_k ? M.H.count[tid * PER + i] : 0;
+        }
+        find_buckets(a, w, c, R, L);                     // (the histogram's place is free behind its barriers)
+        const Classes in(R);
+        z.each([&](float x, int j) {
+            if (masked(x)) return;
+            const int b = bucket_of(x, top, a.bucket_scale);
+            if (b < in.sure) {
+                const double y = weight_of(x, top, a.inv_t);
+                if (y >= a.min_p) mine += whole(y, a.weight_bits);
+            } else if (in.listed(b)) {
+                M.T.put(a, atomicAdd(&n_listed, 1), x, j, top);
+            }
+        });
+        __syncthreads();
+        const int n = n_listed;                          // (a segment's ids: they fit)
+        const Entries E{z.z, nullptr, -1, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
+        kept.least = find_least(a, R, E, M.T, n, top, SL, L);
+        for (int i = tid; i < n; i += NT)
+            if (M.T.key[i] >= kept.least) mine += whole(kept(logit_of(M.T.key[i]), id_of(M.T.key[i])), a.weight_bits);
+    } else {
+        z.each([&](float x, int) {
+            if (masked(x)) return;
+            const double y = weight_of(x, top, a.inv_t);
+            if (y >= a.min_p) mine += whole(y, a.weight_bits);
+        });
+    }
+    mine = block_sum(mine, L);
+    if (a.tok_out) {
+        draw_and_report(a, kept, z.z, tid == 0 ? mine : 0, K, L);
+        return;
+    }
+    const uint64_t total = outcome(a, r, top, kept.least, tid == 0 ? mine : 0, L);
+    if (probs) {
+        const double inv = 1.0 / ldexp((double)total, -a.weight_bits);
+        z.each([&](float x, int j) {
+            if (j < a.V) probs[(size_t)r * a.V + j] = (float)(kept(x, j) * inv);
+        });
     }
 }
 
@@ -566,14 +823,17 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
 // the distributions
 // ---------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(NT) k_filter_probs(FilterArgs a, float *probs) {
-    const int r = blockIdx.y, j0 = blockIdx.x * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids);
-    const float *z = row_of(a, r);
+    const int r = blockIdx.y;
+    SegLogits z;
+    z.load(a, r, blockIdx.x);
     float *p = probs + (size_t)r * a.V;
     const FilterRow &R = a.s->row[r];
     const Kept kept{R.least, R.top, a.inv_t, a.min_p};
     const double inv = 1.0 / ldexp((double)R.total, -a.weight_bits);
     const bool bad = R.bad;
-    for (int j = j0 + (int)threadIdx.x; j < j1; j += NT) p[j] = bad ? __uint_as_float(0x7fc00000u) : (float)(kept(z[j], j) * inv);
+    z.each([&](float x, int j) {
+        if (j < z.j1) p[j] = bad ? __uint_as_float(0x7fc00000u) : (float)(kept(x, j) * inv);
+    });
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -641,12 +901,21 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             for (int w = 0; w < NW; ++w) c = fmax(c, top_of[w]);
             return c;
         };
-        double c = -INFINITY;
-        for (int j = j0 + tid; j < j1; j += NT) c = fmax(c, res(j));
+        double c = -INFINITY, lw[kKeep];
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            const int j = j0 + tid + i * NT;
+            lw[i] = j < j1 ? res(j) : -INFINITY;
+            c = fmax(c, lw[i]);
+        }
+        for (int j = j0 + tid + kKeep * NT; j < j1; j += NT) c = fmax(c, res(j));
         c = block_max(c);
         uint64_t sum = 0;
-        if (c > -INFINITY)
-            for (int j = j0 + tid; j < j1; j += NT) sum += whole(exp(res(j) - c), a.weight_bits);
+        if (c > -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) sum += whole(exp(lw[i] - c), a.weight_bits);
+            for (int j = j0 + tid + kKeep * NT; j < j1; j += NT) sum += whole(exp(res(j) - c), a.weight_bits);
+        }
         sum = block_sum(sum, L);
         if (tid == 0) {
             leave(&S.res[2 * blockIdx.x], __builtin_bit_cast(uint64_t, c));
@@ -710,9 +979,11 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
     }
 }
 
-int launch_rows(const FilterArgs &a, const LaunchCtx &c) {
+// probs: null, or where rows of one segment are written (others: k_filter_probs)
+int launch_rows(const FilterArgs &a, const LaunchCtx &c, float *probs = nullptr) {
     if (a.V < 1 || a.rows < 1 || a.rows > kFilterRows || a.n_seg > kFilterMaxSegs || !(a.inv_t > 0.0)) return (int)hipErrorInvalidValue;
     const dim3 grid(a.n_seg, a.rows), wg(NT);
+    if (a.n_seg == 1) return launch<k_filter_one>(c, dim3(a.rows), wg, 0, a, probs);
     int rc = launch<k_filter_top>(c, grid, wg, 0, a);
     if (rc) return rc;
     if (a.top_k || a.top_p < 1.0) {
@@ -744,8 +1015,8 @@ int launch_filter_sample(const FilterArgs &a, const LaunchCtx &c) {
 
 int launch_filter_probs(const FilterArgs &a, float *probs, const LaunchCtx &c) {
     if (a.tok_out) return (int)hipErrorInvalidValue;
-    const int rc = launch_rows(a, c);
-    return rc ? rc : launch<k_filter_probs>(c, dim3(a.n_seg, a.rows), dim3(NT), 0, a, probs);
+    const int rc = launch_rows(a, c, probs);
+    return rc || a.n_seg == 1 ? rc : launch<k_filter_probs>(c, dim3(a.n_seg, a.rows), dim3(NT), 0, a, probs);
 }
 
 int launch_filter_verify(const FilterVerifyArgs &v, const LaunchCtx &c) {
