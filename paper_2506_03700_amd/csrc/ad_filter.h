@@ -12,7 +12,7 @@ constexpr int kFilterSegIds = 2048;                  // ids per segment, until t
 constexpr int kFilterMaxSegs = kFilterThreads;
 constexpr int kFilterBuckets = 2048;                 // of logits, by their distance from the row's largest
 constexpr int kFilterRows = 15;                      // 8 final and 7 draft rows of a verification
-constexpr int kFilterList = 8192;                    // entries of the buckets that a boundary lies in, that a row's list holds
+constexpr int kFilterList = 4096;                    // ids of the buckets that a boundary lies in, that a row's list has places for
 
 // What the kernels leave one another, for one row.
 struct FilterRow {
@@ -28,13 +28,12 @@ struct FilterRow {
     float top;                                       // largest logit
     int bad;                                         // no distribution: a logit is no number or plus infinity, or all are minus infinity
 };
-struct FilterScratch {                               // dev; histograms, list lengths and arrivals are zero between calls
+struct FilterScratch {                               // dev; histograms and arrivals are zero between calls
     uint64_t weight[kFilterRows][kFilterBuckets];
     uint32_t count[kFilterRows][kFilterBuckets];
     float seg_top[kFilterRows][kFilterMaxSegs];
     uint64_t seg_weight[kFilterRows][kFilterMaxSegs];
-    uint64_t list[kFilterRows][kFilterList];         // logit's bits, id
-    uint32_t list_n[kFilterRows][32];                // (a line each)
+    uint64_t list[kFilterRows][kFilterList];         // per segment: logit's bits, id
     uint32_t arrivals[kFilterRows + 1][32];
     FilterRow row[kFilterRows];
     uint64_t res[2 * kFilterMaxSegs];                // residual, per segment: the bits of the logarithm of its largest weight, its weight
@@ -43,6 +42,7 @@ struct FilterScratch {                               // dev; histograms, list le
 struct FilterArgs {
     const float *z0, *z1;                            // dev: rows 0 .. n_first - 1, then the others; [V] each
     int n_first, rows, V, n_seg, seg_ids;
+    int places;                                      // of a segment in its row's list
     int top_k;                                       // 0: off
     double inv_t, top_p, min_p;                      // 1 / temperature; 1: off; 0: off
     float bucket_scale;                              // 64 / temperature

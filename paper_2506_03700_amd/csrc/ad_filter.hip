@@ -30,7 +30,7 @@ namespace {
 constexpr int NT = kFilterThreads, NW = NT / 64;
 constexpr int kRank = 64;                                // entries that are ranked against each other
 constexpr int kKeep = kFilterSegIds / NT;                // logits that a thread keeps (longer segments read the others again)
-constexpr int kEntries = 2048;                           // entries of a list that are taken into LDS
+constexpr uint64_t kUnused = ~0ull, kTooMany = ~0ull - 1; // in places of a list (no listed logit has these bits)
 constexpr int kLinear = 1792;                            // buckets of equal width
 
 // ---------------------------------------------------------------------------------------------------
@@ -67,8 +67,7 @@ __device__ __forceinline__ const float *row_of(const FilterArgs &a, int r) {
 // ---------------------------------------------------------------------------------------------------
 struct BlockLds {
     float f[NW];
-    uint64_t u[NW];
-    uint64_t total;
+    uint64_t u[NW], u2[NW];
     int last_wg;
 };
 // maximum over the workgroup; not a number if one of the values is none
@@ -117,6 +116,29 @@ __device__ __forceinline__ uint64_t block_scan(uint64_t v, BlockLds &L, uint64_t
     *total = all;
     return before + in - v;
 }
+// of two numbers at once
+__device__ __forceinline__ void block_scan2(uint64_t &v, uint64_t &u, BlockLds &L, uint64_t *total_v, uint64_t *total_u) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t in = wave_scan(v, lane), iu = wave_scan(u, lane);
+    __syncthreads();
+    if (lane == 63) {
+        L.u[wave] = in;
+        L.u2[wave] = iu;
+    }
+    __syncthreads();
+    uint64_t before = 0, all = 0, before2 = 0, all2 = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        before += w < wave ? L.u[w] : 0;
+        all += L.u[w];
+        before2 += w < wave ? L.u2[w] : 0;
+        all2 += L.u2[w];
+    }
+    *total_v = all;
+    *total_u = all2;
+    v = before + in - v;
+    u = before2 + iu - u;
+}
 __device__ __forceinline__ uint64_t block_sum(uint64_t v, BlockLds &L) {
     uint64_t all;
     (void)block_scan(v, L, &all);
@@ -139,7 +161,6 @@ __device__ __forceinline__ uint64_t block_extreme(uint64_t v, BlockLds &L) {
 }
 
 __device__ __forceinline__ uint64_t seen(const uint64_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ uint32_t seen(const uint32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <class T>
 __device__ __forceinline__ void leave(T *p, T v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // the last workgroup of n on this counter, when everything that any wavefront of any of them has left is in memory
@@ -193,10 +214,25 @@ __global__ void __launch_bounds__(NT) k_filter_top(FilterArgs a) {
     if (threadIdx.x == 0) a.s->seg_top[blockIdx.y][blockIdx.x] = m;
 }
 
-// of the row, to every thread; *bad: it has no distribution
-__device__ __forceinline__ float row_top(const FilterArgs &a, int r, BlockLds &L, bool *bad) {
-    const float m = block_top((int)threadIdx.x < a.n_seg ? a.s->seg_top[r][threadIdx.x] : -INFINITY, L);
-    *bad = !(fabsf(m) < INFINITY);
+// of the row, to every thread (every wavefront looks at all segments, which saves the barriers); *bad: it has no distribution
+__device__ __forceinline__ float row_top(const FilterArgs &a, int r, bool *bad) {
+    constexpr int PER = kFilterMaxSegs / 64;
+    const int lane = threadIdx.x & 63;
+    const float *seg = a.s->seg_top[r];
+    float m = lane < a.n_seg ? seg[lane] : -INFINITY;
+    bool nan = m != m;
+    if (a.n_seg > 64) {
+        float v[PER - 1];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) v[i - 1] = lane + 64 * i < a.n_seg ? seg[lane + 64 * i] : -INFINITY;
+#pragma unroll
+        for (int i = 1; i < PER; ++i) {
+            nan |= v[i - 1] != v[i - 1];
+            m = fmaxf(m, v[i - 1]);
+        }
+    }
+    m = max64(m);
+    *bad = __any(nan) || !(fabsf(m) < INFINITY);
     return m;
 }
 
@@ -227,11 +263,11 @@ __device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t
     constexpr int PER = kFilterBuckets / NT;
     const int tid = threadIdx.x;
     __shared__ uint64_t in_k;
-    uint64_t ws = 0, cs = 0, w0 = 0, c0 = 0, all_w = 0, all_c = 0;
+    uint64_t w0 = 0, c0 = 0, all_w = 0, all_c = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        ws += w[i];
-        cs += c[i];
+        w0 += w[i];
+        c0 += c[i];
     }
     if (tid == 0) {
         R.p0 = kFilterBuckets;
@@ -241,8 +277,7 @@ __device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t
         R.weight_p = R.weight_k = 0;
         in_k = 0;
     }
-    if (a.top_p < 1.0) w0 = block_scan(ws, L, &all_w);
-    if (a.top_k) c0 = block_scan(cs, L, &all_c);
+    block_scan2(w0, c0, L, &all_w, &all_c);
     if (tid == 0) R.weight = all_w;
     // top-k: the bucket of the last id it keeps (none if it keeps them all)
     if (a.top_k && (uint64_t)a.top_k < all_c) {
@@ -291,7 +326,8 @@ __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
     z.load(a, r, blockIdx.x);
     H.clear(a);
     bool bad;
-    const float top = row_top(a, r, L, &bad);
+    const float top = row_top(a, r, &bad);
+    __syncthreads();
     if (!bad) z.each([&](float x, int) { H.add(a, x, top); });
     __syncthreads();
     for (int b = tid; b < kFilterBuckets; b += NT) {
@@ -305,12 +341,16 @@ __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         w[i] = a.top_p < 1.0 ? seen(&S.weight[r][tid * PER + i]) : 0;
-        c[i] = a.top_k ? seen(&S.count[r][tid * PER + i]) : 0;
+        if ((i & 1) == 0) {                              // (two counts to a load)
+            const uint64_t two = a.top_k ? seen((const uint64_t *)&S.count[r][tid * PER + i]) : 0;
+            c[i] = (uint32_t)two;
+            c[i + 1] = (uint32_t)(two >> 32);
+        }
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {                      // zero for the next call
         if (a.top_p < 1.0) leave(&S.weight[r][tid * PER + i], (uint64_t)0);
-        if (a.top_k) leave(&S.count[r][tid * PER + i], 0u);
+        if (a.top_k && (i & 1) == 0) leave((uint64_t *)&S.count[r][tid * PER + i], (uint64_t)0);
     }
     find_buckets(a, w, c, R, L);
     if (tid == 0) S.row[r] = R;
@@ -319,26 +359,17 @@ __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
 // ---------------------------------------------------------------------------------------------------
 // 3. the rows' outcomes
 // ---------------------------------------------------------------------------------------------------
-// The entries that a boundary is looked for among: the row's list or, if more ids lie in those buckets than it holds, the row itself.
+// The ids of a row that lie in some buckets, straight from its logits: where a boundary is looked for if there are more of them than the list has places.
 struct Entries {
     const float *z;
-    const uint64_t *list;
-    int n;                                               // length of the list; < 0: the row
     int V, weight_bits;
     float top, scale;
     double inv_t;
-    __device__ __forceinline__ int count() const { return n >= 0 ? n : V; }
-    // the i-th, if it is one of buckets b0 .. b1
-    __device__ __forceinline__ bool get(int i, int b0, int b1, float &x, int &id) const {
-        if (n >= 0) {
-            const uint64_t e = seen(list + i);
-            x = __uint_as_float((uint32_t)(e >> 32));
-            id = (int)(uint32_t)e;
-        } else {
-            x = z[i];
-            id = i;
-            if (masked(x)) return false;
-        }
+    __device__ __forceinline__ int count() const { return V; }
+    // logit of id i, if it is one of buckets b0 .. b1
+    __device__ __forceinline__ bool get(int i, int b0, int b1, float &x) const {
+        x = z[i];
+        if (masked(x)) return false;
         const int b = bucket_of(x, top, scale);
         return b >= b0 && b <= b1;
     }
@@ -348,8 +379,8 @@ struct SelectLds {
     uint64_t m[NT];                                      // measure, or weight, by bin
     uint32_t c[NT];                                      // entries by bin
     uint64_t key[kRank], w[kRank];                       // the entries that are ranked
-    int n, bin, bin_n;
-    uint64_t before, before_w;
+    int n, bin;
+    uint64_t before;
 };
 
 // The ids of buckets b0 .. b1 in their order; an id is kept if the measures (1 each, or the weights) of the ones before it add up to less than `limit`.
@@ -361,9 +392,8 @@ __device__ uint64_t least_kept(const Entries &E, int b0, int b1, uint64_t limit,
     uint64_t lo = ~0ull, hi = 0, cnt = 0;
     for (int i = tid; i < N; i += NT) {
         float x;
-        int id;
-        if (!E.get(i, b0, b1, x, id)) continue;
-        const uint64_t k = key_of(x, id);
+        if (!E.get(i, b0, b1, x)) continue;
+        const uint64_t k = key_of(x, i);
         lo = k < lo ? k : lo;
         hi = k > hi ? k : hi;
         ++cnt;
@@ -382,9 +412,8 @@ __device__ uint64_t least_kept(const Entries &E, int b0, int b1, uint64_t limit,
         __syncthreads();
         for (int i = tid; i < N; i += NT) {
             float x;
-            int id;
-            if (!E.get(i, b0, b1, x, id)) continue;
-            const uint64_t k = key_of(x, id);
+            if (!E.get(i, b0, b1, x)) continue;
+            const uint64_t k = key_of(x, i);
             if (k < lo || k > hi) continue;
             const int bin = (int)((hi - k) >> shift);
             atomicAdd(&S.c[bin], 1u);
@@ -412,9 +441,8 @@ __device__ uint64_t least_kept(const Entries &E, int b0, int b1, uint64_t limit,
     __syncthreads();
     for (int i = tid; i < N; i += NT) {
         float x;
-        int id;
-        if (!E.get(i, b0, b1, x, id)) continue;
-        const uint64_t k = key_of(x, id);
+        if (!E.get(i, b0, b1, x)) continue;
+        const uint64_t k = key_of(x, i);
         if (k < lo || k > hi) continue;
         const int at = atomicAdd(&S.n, 1);
         S.key[at] = k;
@@ -431,71 +459,71 @@ __device__ uint64_t least_kept(const Entries &E, int b0, int b1, uint64_t limit,
     return block_extreme<false>(least, L);
 }
 
-// A list in LDS: keys, weights and buckets of its entries.
-struct EntryLds {
-    uint64_t key[kEntries], w[kEntries];
-    uint16_t bucket[kEntries];
-    __device__ __forceinline__ void put(const FilterArgs &a, int at, float x, int id, float top) {
-        key[at] = key_of(x, id);
-        w[at] = whole(weight_of(x, top, a.inv_t), a.weight_bits);
-        bucket[at] = (uint16_t)bucket_of(x, top, a.bucket_scale);
-    }
-};
 __device__ __forceinline__ float logit_of(uint64_t key) {
     const uint32_t u = (uint32_t)(key >> 32);
     return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 __device__ __forceinline__ int id_of(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 
-// least_kept for the common case, a list in LDS: the buckets of equal width cut once more into NT bins, and no more than kRank entries in the boundary's bin, which
-// every wavefront ranks for itself.  False if it is not that case.  *weight: of what is kept (for counts; the weights are measured too).
+// least_kept for the common case, n keys in LDS: the buckets of equal width cut once more into 128 bins, two to a lane of every wavefront, and no more than kRank
+// entries in the boundary's bin, which every wavefront ranks for itself: two barriers in all.  False if it is not that case.  *weight: of what is kept (for
+// counts; the weights are measured too).
 template <bool WEIGHTS>
-__device__ __forceinline__ bool least_kept_lds(const FilterArgs &a, const EntryLds &T, int n, int b0, int b1, uint64_t limit, float top, SelectLds &S, BlockLds &L,
+__device__ __forceinline__ bool least_kept_lds(const FilterArgs &a, const uint64_t *T, int n, int b0, int b1, uint64_t limit, float top, SelectLds &S,
                                                uint64_t *least, uint64_t *weight) {
+    constexpr int kBins = 128;
     const int tid = threadIdx.x, lane = tid & 63;
     if (b1 >= kLinear || limit == 0) return false;
-    const float fine = (float)NT / (float)(b1 - b0 + 1);
-    auto bin_of = [&](int i) {                           // (monotonic in the logit)
-        float x = (top - logit_of(T.key[i])) * a.bucket_scale;
+    const float fine = (float)kBins / (float)(b1 - b0 + 1);
+    auto bin_of = [&](float z) {                         // (monotonic in the logit); negative: of another bucket
+        const int in = bucket_of(z, top, a.bucket_scale);
+        float x = (top - z) * a.bucket_scale;
         asm("" : "+v"(x));                               // (the same rounding both times)
         const int b = (int)((x - (float)b0) * fine);
-        return b < 0 ? 0 : b < NT ? b : NT - 1;
+        return in < b0 || in > b1 ? -1 : b < 0 ? 0 : b < kBins ? b : kBins - 1;
     };
+    auto weight_at = [&](float z) { return whole(weight_of(z, top, a.inv_t), a.weight_bits); };
     __syncthreads();
-    S.m[tid] = 0;
-    S.c[tid] = 0;
-    if (tid == 0) S.n = S.bin = 0;
+    if (tid < kBins) {
+        S.m[tid] = 0;
+        S.c[tid] = 0;
+    }
+    if (tid == 0) S.n = 0;
     __syncthreads();
     for (int i = tid; i < n; i += NT) {
-        if (T.bucket[i] < b0 || T.bucket[i] > b1) continue;
-        const int b = bin_of(i);
+        const float z = logit_of(T[i]);
+        const int b = bin_of(z);
+        if (b < 0) continue;
         atomicAdd(&S.c[b], 1u);
-        atomicAdd((unsigned long long *)&S.m[b], (unsigned long long)T.w[i]);
+        atomicAdd((unsigned long long *)&S.m[b], (unsigned long long)weight_at(z));
     }
     __syncthreads();
-    uint64_t all, before_c = 0;
-    const uint64_t before_w = block_scan(S.m[tid], L, &all);
-    if (!WEIGHTS) before_c = block_scan(S.c[tid], L, &all);
-    const uint64_t before = WEIGHTS ? before_w : before_c;
-    if (S.c[tid] && before < limit) atomicMax(&S.bin, tid);
-    __syncthreads();
-    const int bin = S.bin;
-    if (tid == bin) {
-        S.before = before;
-        S.before_w = before_w;
-        S.bin_n = (int)S.c[tid];
+    // lane l: bins 2 l and 2 l + 1; the last bin with entries before which the measures stay below the limit
+    const uint32_t c0 = S.c[2 * lane], c1 = S.c[2 * lane + 1];
+    const uint64_t m0 = S.m[2 * lane], m1 = S.m[2 * lane + 1];
+    const uint64_t w0 = wave_scan(m0 + m1, lane) - (m0 + m1), w1 = w0 + m0;
+    uint64_t at0 = w0, at1 = w1;
+    if (!WEIGHTS) {
+        at0 = wave_scan((uint64_t)c0 + c1, lane) - ((uint64_t)c0 + c1);
+        at1 = at0 + c0;
     }
-    __syncthreads();
-    const int nb = S.bin_n;
-    if (nb > kRank || nb == 0) return false;
+    const unsigned long long in0 = __ballot(c0 && at0 < limit), in1 = __ballot(c1 && at1 < limit);
+    const int l0 = 63 - __clzll(in0), l1 = 63 - __clzll(in1);            // (-1: none)
+    if (l0 < 0 && l1 < 0) return false;
+    const bool odd = l1 >= l0;
+    const int l = odd ? l1 : l0, bin = 2 * l + odd;
+    const int nb = __builtin_amdgcn_readlane((int)(odd ? c1 : c0), l);
+    const uint64_t before = lane_u64(odd ? at1 : at0, l), before_w = lane_u64(odd ? w1 : w0, l);
+    if (nb > kRank) return false;
     for (int i = tid; i < n; i += NT) {
-        if (T.bucket[i] < b0 || T.bucket[i] > b1 || bin_of(i) != bin) continue;
+        const float z = logit_of(T[i]);
+        if (bin_of(z) != bin) continue;
         const int at = atomicAdd(&S.n, 1);
-        S.key[at] = T.key[i];
-        S.w[at] = T.w[i];
+        S.key[at] = T[i];
+        S.w[at] = weight_at(z);
     }
     __syncthreads();
-    const uint64_t mine = lane < nb ? S.key[lane] : 0, left = limit - S.before;
+    const uint64_t mine = lane < nb ? S.key[lane] : 0, left = limit - before;
     uint64_t ahead = 0;
     int rank = 0;
     for (int i = 0; i < nb; ++i) {
@@ -506,7 +534,7 @@ __device__ __forceinline__ bool least_kept_lds(const FilterArgs &a, const EntryL
     const bool kept = lane < nb && ahead < left;
     const int n_kept = __popcll(__ballot(kept));         // one at least: nothing is ahead of the first
     *least = lane_u64(mine, __ffsll(__ballot(lane < nb && rank == n_kept - 1)) - 1);
-    *weight = S.before_w + lane_u64(wave_scan(kept ? S.w[lane] : 0, lane), 63);
+    *weight = before_w + lane_u64(wave_scan(kept ? S.w[lane] : 0, lane), 63);
     return true;
 }
 
@@ -524,10 +552,10 @@ struct Kept {
 };
 
 struct WalkLds { int hit, seg; uint64_t before; double w; };
-// The id that a draw falls on, by inversion over weights w(j) >= 0 in id order, in segments whose weights (multiples of 2^-bits, as w's) thread t holds of segment t:
-// in every thread; *weight: w of it.  The total is not zero.
-template <class W>
-__device__ int draw(const FilterArgs &a, uint64_t mine, float u, W w, WalkLds &K, BlockLds &L, double *weight, uint64_t *sum) {
+// The id that a draw falls on, by inversion over the kept ids of row z in id order, thread t having the weight of segment t: in every thread;
+// *weight: that id's, *sum: the row's, which is not zero.
+__device__ __forceinline__ int draw(const FilterArgs &a, uint64_t mine, float u, const Kept &kept, const float *z, WalkLds &K, BlockLds &L, double *weight,
+                                    uint64_t *sum) {
     const int tid = threadIdx.x;
     uint64_t total, ignore;
     const uint64_t before = block_scan(mine, L, &total);
@@ -537,24 +565,41 @@ __device__ int draw(const FilterArgs &a, uint64_t mine, float u, W w, WalkLds &K
         K.seg = tid;
         K.before = before;
     }
-    if (tid == 0) K.hit = 0x7fffffff;
     __syncthreads();
+    // thread t has consecutive ids of the segment, the logits of the first kKeep of them all on their way at once
     const int seg = K.seg, j0 = seg * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids), per = (a.seg_ids + NT - 1) / NT;
     const int i0 = min(j1, j0 + tid * per), i1 = min(j1, i0 + per);
+    float v[kKeep];
+    double x[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) v[i] = i0 + i < i1 ? z[i0 + i] : -INFINITY;
     uint64_t own = 0;
-    for (int j = i0; j < i1; ++j) own += whole(w(j), a.weight_bits);
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+        x[i] = kept(v[i], i0 + i);
+        own += whole(x[i], a.weight_bits);
+    }
+    for (int j = i0 + kKeep; j < i1; ++j) own += whole(kept(z[j], j), a.weight_bits);
     const uint64_t at = K.before + block_scan(own, L, &ignore);
     if (at <= target && target < at + own) {
         uint64_t c = at;
-        for (int j = i0; j < i1; ++j) {
-            const double x = w(j);
-            c += whole(x, a.weight_bits);
-            if (c > target) {
-                K.hit = j;
-                K.w = x;
-                break;
+        int hit = -1;
+        double w_hit = 0.0;
+#pragma unroll
+        for (int i = 0; i < kKeep; ++i) {
+            c += whole(x[i], a.weight_bits);
+            if (hit < 0 && c > target) {
+                hit = i0 + i;
+                w_hit = x[i];
             }
         }
+        for (int j = i0 + kKeep; j < i1 && hit < 0; ++j) {
+            w_hit = kept(z[j], j);
+            c += whole(w_hit, a.weight_bits);
+            if (c > target) hit = j;
+        }
+        K.hit = hit;
+        K.w = w_hit;
     }
     __syncthreads();
     *weight = K.w;
@@ -569,19 +614,18 @@ __device__ __forceinline__ void report_draw(const FilterArgs &a, int tok, float 
     report_done(a.done_flag, a.done_seq);
 }
 
-// The smallest key that top-k and top-p keep, R saying which buckets their boundaries lie in.  n: entries in T, negative if they are not there.
-__device__ __forceinline__ uint64_t find_least(const FilterArgs &a, const FilterRow &R, const Entries &E, const EntryLds &T, int n, float top, SelectLds &S, BlockLds &L) {
+// The smallest key that top-k and top-p keep, R saying which buckets their boundaries lie in.  T: the n keys of those buckets, in LDS (negative: they are not there).
+__device__ __forceinline__ uint64_t find_least(const FilterArgs &a, const FilterRow &R, const Entries &E, const uint64_t *T, int n, float top, SelectLds &S, BlockLds &L) {
     uint64_t least = 0, weight = R.weight;
     if (R.bk >= 0) {
         const uint64_t limit = (uint64_t)a.top_k - R.count_k;
         uint64_t in_bucket;
-        if (n < 0 || !least_kept_lds<false>(a, T, n, R.bk, R.bk, limit, top, S, L, &least, &in_bucket)) {
+        if (n < 0 || !least_kept_lds<false>(a, T, n, R.bk, R.bk, limit, top, S, &least, &in_bucket)) {
             least = least_kept<false>(E, R.bk, R.bk, limit, S, L);
             in_bucket = 0;
             for (int i = threadIdx.x; i < E.count(); i += NT) {
                 float x;
-                int id;
-                if (E.get(i, R.bk, R.bk, x, id) && key_of(x, id) >= least) in_bucket += whole(weight_of(x, top, a.inv_t), a.weight_bits);
+                if (E.get(i, R.bk, R.bk, x) && key_of(x, i) >= least) in_bucket += whole(weight_of(x, top, a.inv_t), a.weight_bits);
             }
             in_bucket = block_sum(in_bucket, L);
         }
@@ -591,7 +635,7 @@ __device__ __forceinline__ uint64_t find_least(const FilterArgs &a, const Filter
         // kept: less than top_p * weight before it
         const uint64_t bound = (uint64_t)ceil(a.top_p * (double)weight), limit = bound > R.weight_p ? bound - R.weight_p : 0;
         uint64_t by_p, ignore;
-        if (n < 0 || !least_kept_lds<true>(a, T, n, R.p0, R.p1, limit, top, S, L, &by_p, &ignore)) by_p = least_kept<true>(E, R.p0, R.p1, limit, S, L);
+        if (n < 0 || !least_kept_lds<true>(a, T, n, R.p0, R.p1, limit, top, S, &by_p, &ignore)) by_p = least_kept<true>(E, R.p0, R.p1, limit, S, L);
         least = by_p > least ? by_p : least;
     }
     return least;
@@ -632,7 +676,7 @@ __device__ __forceinline__ uint64_t outcome(const FilterArgs &a, int r, float to
 __device__ __forceinline__ void draw_and_report(const FilterArgs &a, const Kept &kept, const float *z, uint64_t w, WalkLds &K, BlockLds &L) {
     double x;
     uint64_t total;
-    const int tok = draw(a, w, a.u, [&](int j) { return kept(z[j], j); }, K, L, &x, &total);
+    const int tok = draw(a, w, a.u, kept, z, K, L, &x, &total);
     if (threadIdx.x == 0) report_draw(a, tok, (float)(x / ldexp((double)total, -a.weight_bits)));
 }
 
@@ -641,10 +685,10 @@ template <bool BOUND>
 __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     __shared__ BlockLds L;
     __shared__ SelectLds SL;
-    __shared__ EntryLds T;
+    __shared__ uint64_t T[kFilterList];
     __shared__ WalkLds K;
     __shared__ uint64_t seg_w[kFilterMaxSegs];
-    __shared__ int n_mine, at_mine;
+    __shared__ int n_mine;
     const int r = blockIdx.y, tid = threadIdx.x;
     FilterScratch &S = *a.s;
     SegLogits z;
@@ -659,7 +703,8 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     const Classes in(R);
     if (tid == 0) n_mine = 0;
     bool bad;
-    const float top = row_top(a, r, L, &bad);            // (a barrier or two)
+    const float top = row_top(a, r, &bad);
+    if (BOUND) __syncthreads();
     uint64_t mine = 0;
     if (!bad) {
         auto sure = [&](float x) {
@@ -671,33 +716,20 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
                 if (!masked(x)) sure(x);
             });
         } else {
-            auto put = [&](uint32_t at, float x, int j) {
-                if (at < kFilterList) leave(&S.list[r][at], (uint64_t)__float_as_uint(x) << 32 | (uint32_t)j);
-            };
-            unsigned listed = 0;                          // of the kept logits, by their place
-#pragma unroll
-            for (int i = 0; i < kKeep; ++i) {
-                if (masked(z.v[i])) continue;
-                const int b = bucket_of(z.v[i], top, a.bucket_scale);
-                if (b < in.sure) sure(z.v[i]);
-                else listed |= in.listed(b) ? 1u << i : 0;
-            }
-            const int n = __popc(listed);
-            int at = n ? atomicAdd(&n_mine, n) : 0;
-            __syncthreads();
-            if (tid == 0 && n_mine) at_mine = (int)atomicAdd(&S.list_n[r][0], (uint32_t)n_mine);
-            __syncthreads();
-            at += at_mine;
-#pragma unroll
-            for (int i = 0; i < kKeep; ++i)
-                if (listed >> i & 1) put((uint32_t)at++, z.v[i], z.j0 + tid + i * NT);
-            for (int j = z.j0 + tid + kKeep * NT; j < z.j1; j += NT) {           // (segments beyond the usual length)
-                const float x = z.z[j];
-                if (masked(x)) continue;
+            // listed ids go to places of the segment's own (no workgroup waits for a number from another); unused places say so, and the
+            // first one says it if there are too few
+            z.each([&](float x, int j) {
+                if (masked(x)) return;
                 const int b = bucket_of(x, top, a.bucket_scale);
                 if (b < in.sure) sure(x);
-                else if (in.listed(b)) put(atomicAdd(&S.list_n[r][0], 1u), x, j);
-            }
+                else if (in.listed(b)) {
+                    const int at = atomicAdd(&n_mine, 1);
+                    if (at < a.places) T[at] = (uint64_t)__float_as_uint(x) << 32 | (uint32_t)j;
+                }
+            });
+            __syncthreads();
+            if (tid < a.places)
+                leave(&S.list[r][blockIdx.x * a.places + tid], n_mine > a.places ? kTooMany : tid < n_mine ? T[tid] : kUnused);
         }
     }
     mine = block_sum(mine, L);
@@ -711,13 +743,22 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     uint64_t w = tid < a.n_seg ? seen(&S.seg_weight[r][tid]) : 0;
     Kept kept{0, top, a.inv_t, a.min_p};
     if constexpr (BOUND) {
-        const uint32_t n_all = seen(&S.list_n[r][0]);
-        const int n = n_all <= kEntries ? (int)n_all : -1;
-        const Entries E{z.z, S.list[r], n_all <= kFilterList ? (int)n_all : -1, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
-        for (int i = tid; i < n; i += NT) {
-            const uint64_t e = seen(&S.list[r][i]);
-            T.put(a, i, __uint_as_float((uint32_t)(e >> 32)), (int)(uint32_t)e, top);
+        // (every place of the list is on its way before the first is looked at)
+        constexpr int PER = kFilterList / NT;
+        uint64_t e[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) e[i] = tid + i * NT < a.n_seg * a.places ? seen(&S.list[r][tid + i * NT]) : kUnused;
+        if (tid == 0) n_mine = 0;
+        __syncthreads();
+        bool too_many = false;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            too_many |= e[i] == kTooMany;
+            if (e[i] < kTooMany) T[atomicAdd(&n_mine, 1)] = key_of(__uint_as_float((uint32_t)(e[i] >> 32)), (int)(uint32_t)e[i]);
         }
+        too_many = __syncthreads_or(too_many);
+        const int n = too_many ? -1 : n_mine;
+        const Entries E{z.z, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
         kept.least = find_least(a, R, E, T, n, top, SL, L);
         // the listed ones that are kept join their segments
         seg_w[tid] = w;
@@ -728,18 +769,15 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
         };
         if (n >= 0) {
             for (int i = tid; i < n; i += NT)
-                if (T.key[i] >= kept.least) join(logit_of(T.key[i]), id_of(T.key[i]));
+                if (T[i] >= kept.least) join(logit_of(T[i]), id_of(T[i]));
         } else {
             for (int i = tid; i < E.count(); i += NT) {
                 float x;
-                int id;
-                const bool in_p = E.get(i, R.p0, R.p1, x, id);
-                if (in_p || E.get(i, R.bk, R.bk, x, id)) join(x, id);
+                if (E.get(i, R.p0, R.p1, x) || E.get(i, R.bk, R.bk, x)) join(x, i);
             }
         }
         __syncthreads();
         w = seg_w[tid];
-        if (tid == 0) leave(&S.list_n[r][0], 0u);
     }
     if (a.tok_out) draw_and_report(a, kept, z.z, w, K, L);
     else (void)outcome(a, r, top, kept.least, w, L);
@@ -749,7 +787,7 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
 __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
     __shared__ BlockLds L;
     __shared__ SelectLds SL;
-    __shared__ union { Histogram H; EntryLds T; } M;
+    __shared__ union { Histogram H; uint64_t T[kFilterSegIds]; } M;
     __shared__ WalkLds K;
     __shared__ FilterRow R;
     __shared__ int n_listed;
@@ -789,15 +827,15 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
                 const double y = weight_of(x, top, a.inv_t);
                 if (y >= a.min_p) mine += whole(y, a.weight_bits);
             } else if (in.listed(b)) {
-                M.T.put(a, atomicAdd(&n_listed, 1), x, j, top);
+                M.T[atomicAdd(&n_listed, 1)] = key_of(x, j);
             }
         });
         __syncthreads();
         const int n = n_listed;                          // (a segment's ids: they fit)
-        const Entries E{z.z, nullptr, -1, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
+        const Entries E{z.z, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
         kept.least = find_least(a, R, E, M.T, n, top, SL, L);
         for (int i = tid; i < n; i += NT)
-            if (M.T.key[i] >= kept.least) mine += whole(kept(logit_of(M.T.key[i]), id_of(M.T.key[i])), a.weight_bits);
+            if (M.T[i] >= kept.least) mine += whole(kept(logit_of(M.T[i]), id_of(M.T[i])), a.weight_bits);
     } else {
         z.each([&](float x, int) {
             if (masked(x)) return;
@@ -865,6 +903,7 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
     __shared__ BlockLds L;
     __shared__ WalkLds K;
     __shared__ double ratio_of[8], top_of[NW];
+    __shared__ int ids[kFilterSegIds], n_kept;
     const FilterArgs &a = v.f;
     FilterScratch &S = *a.s;
     const int tid = threadIdx.x, n_draft = v.m - 1;
@@ -901,21 +940,24 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             for (int w = 0; w < NW; ++w) c = fmax(c, top_of[w]);
             return c;
         };
-        double c = -INFINITY, lw[kKeep];
-#pragma unroll
-        for (int i = 0; i < kKeep; ++i) {
-            const int j = j0 + tid + i * NT;
-            lw[i] = j < j1 ? res(j) : -INFINITY;
-            c = fmax(c, lw[i]);
-        }
-        for (int j = j0 + tid + kKeep * NT; j < j1; j += NT) c = fmax(c, res(j));
+        // the ids that p keeps, one after the other: few, and the arithmetic behind them is long
+        if (tid == 0) n_kept = 0;
+        __syncthreads();
+        auto each_kept = [&](auto f) {                   // (segments beyond the usual length: their ids as they come)
+            if (a.seg_ids <= kFilterSegIds)
+                for (int i = tid; i < n_kept; i += NT) f(ids[i]);
+            else
+                for (int j = j0 + tid; j < j1; j += NT) f(j);
+        };
+        if (a.seg_ids <= kFilterSegIds)
+            for (int j = j0 + tid; j < j1; j += NT)
+                if (!masked(zp[j]) && key_of(zp[j], j) >= p.kept.least) ids[atomicAdd(&n_kept, 1)] = j;
+        __syncthreads();
+        double c = -INFINITY;
+        each_kept([&](int j) { c = fmax(c, res(j)); });
         c = block_max(c);
         uint64_t sum = 0;
-        if (c > -INFINITY) {
-#pragma unroll
-            for (int i = 0; i < kKeep; ++i) sum += whole(exp(lw[i] - c), a.weight_bits);
-            for (int j = j0 + tid + kKeep * NT; j < j1; j += NT) sum += whole(exp(res(j) - c), a.weight_bits);
-        }
+        if (c > -INFINITY) each_kept([&](int j) { sum += whole(exp(res(j) - c), a.weight_bits); });
         sum = block_sum(sum, L);
         if (tid == 0) {
             leave(&S.res[2 * blockIdx.x], __builtin_bit_cast(uint64_t, c));
@@ -967,7 +1009,7 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
     }
     if (tok < 0 && !bad) {   // nothing rejected, or a residual that is identically zero: the row's own distribution
         const uint64_t w = tid < a.n_seg ? S.seg_weight[r][tid] : 0;
-        tok = draw(a, w, rejected ? v.u_resample[r] : v.u_final, [&](int j) { return p.kept(zp[j], j); }, K, L, &x, &total);
+        tok = draw(a, w, rejected ? v.u_resample[r] : v.u_final, p.kept, zp, K, L, &x, &total);
     }
     if (tid < 64) {
         if (v.ratio_out && tid < n_draft) report(v.ratio_out + tid, tid <= r ? (float)ratio_of[tid] : 0.f);
@@ -999,6 +1041,7 @@ void filter_finish(FilterArgs &a, float temperature, int top_k, float top_p, flo
     const int n = (a.V + kFilterSegIds - 1) / kFilterSegIds, most = n < kFilterMaxSegs ? n : kFilterMaxSegs;
     a.seg_ids = (a.V + most - 1) / most;
     a.n_seg = (a.V + a.seg_ids - 1) / a.seg_ids;
+    a.places = kFilterList / a.n_seg < 64 ? kFilterList / a.n_seg : 64;
     a.inv_t = 1.0 / (double)temperature;
     a.bucket_scale = 64.0 * a.inv_t < 3e38 ? (float)(64.0 * a.inv_t) : 3e38f;
     a.top_k = top_k < a.V ? top_k : 0;
