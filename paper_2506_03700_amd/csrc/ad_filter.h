@@ -45,6 +45,7 @@ struct FilterArgs {
     int places;                                      // of a segment in its row's list
     int top_k;                                       // 0: off
     double inv_t, top_p, min_p;                      // 1 / temperature; 1: off; 0: off
+    double min_x;                                    // temperature * log(min_p), near enough
     float bucket_scale;                              // 64 / temperature
     int weight_bits;                                 // weights are multiples of 2^-weight_bits of the largest
     FilterScratch *s;

@@ -542,14 +542,49 @@ __device__ __forceinline__ bool least_kept_lds(const FilterArgs &a, const uint64
 struct Kept {
     uint64_t least;
     float top;
-    double inv_t, min_p;
+    double inv_t;
+    __device__ __forceinline__ bool holds(float x, int id) const { return !masked(x) && key_of(x, id) >= least; }
     // weight in 64 bits, 0 if it is not kept
-    __device__ __forceinline__ double operator()(float x, int id) const {
-        if (masked(x) || key_of(x, id) < least) return 0.0;
-        const double w = weight_of(x, top, inv_t);
-        return w >= min_p ? w : 0.0;
-    }
+    __device__ __forceinline__ double operator()(float x, int id) const { return holds(x, id) ? weight_of(x, top, inv_t) : 0.0; }
 };
+
+// The smallest key that min-p keeps: that of the smallest logit whose weight is at least min_p.  It lies within a step or two of top + min_x; the search goes as far as
+// it has to (weights that are all 1 at a temperature beyond the logits' range).
+__device__ uint64_t least_by_weight(const FilterArgs &a, float top) {
+    if (a.min_p == 0.0) return 0;
+    auto kept = [&](uint32_t u) { return weight_of(__uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u), top, a.inv_t) >= a.min_p; };
+    const uint32_t first = 0x00800000u, last = (uint32_t)(key_of(top, 0) >> 32);         // of the smallest finite number, of the top (which is kept)
+    uint32_t u = (uint32_t)(key_of((float)fmax((double)top + a.min_x, -3.4028234663852886e38), 0) >> 32), no, yes;
+    u = u < last ? u : last;
+    if (kept(u)) {
+        yes = u;
+        for (uint32_t s = 1;; s *= 2) {
+            if (yes - first <= s) {
+                if (kept(first)) return (uint64_t)first << 32;
+                no = first;
+                break;
+            }
+            if (!kept(yes - s)) {
+                no = yes - s;
+                break;
+            }
+            yes -= s;
+        }
+    } else {
+        no = u;
+        for (uint32_t s = 1;; s *= 2) {
+            yes = last - no <= s ? last : no + s;
+            if (yes == last || kept(yes)) break;
+            no = yes;
+        }
+    }
+    while (yes - no > 1) {
+        const uint32_t mid = no + (yes - no) / 2;
+        if (kept(mid)) yes = mid;
+        else no = mid;
+    }
+    return (uint64_t)yes << 32;                          // whatever the id
+}
 
 struct WalkLds { int hit, seg; uint64_t before; double w; };
 // The id that a draw falls on, by inversion over the kept ids of row z in id order, thread t having the weight of segment t: in every thread;
@@ -741,7 +776,7 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
         return;
     }
     uint64_t w = tid < a.n_seg ? seen(&S.seg_weight[r][tid]) : 0;
-    Kept kept{0, top, a.inv_t, a.min_p};
+    Kept kept{least_by_weight(a, top), top, a.inv_t};
     if constexpr (BOUND) {
         // (every place of the list is on its way before the first is looked at)
         constexpr int PER = kFilterList / NT;
@@ -759,7 +794,8 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
         too_many = __syncthreads_or(too_many);
         const int n = too_many ? -1 : n_mine;
         const Entries E{z.z, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
-        kept.least = find_least(a, R, E, T, n, top, SL, L);
+        const uint64_t least = find_least(a, R, E, T, n, top, SL, L);
+        kept.least = least > kept.least ? least : kept.least;
         // the listed ones that are kept join their segments
         seg_w[tid] = w;
         __syncthreads();
@@ -802,7 +838,7 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
         });
         return;
     }
-    Kept kept{0, top, a.inv_t, a.min_p};
+    Kept kept{least_by_weight(a, top), top, a.inv_t};
     uint64_t mine = 0;
     if (a.top_k || a.top_p < 1.0) {
         M.H.clear(a);
@@ -833,7 +869,8 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
         __syncthreads();
         const int n = n_listed;                          // (a segment's ids: they fit)
         const Entries E{z.z, a.V, a.weight_bits, top, a.bucket_scale, a.inv_t};
-        kept.least = find_least(a, R, E, M.T, n, top, SL, L);
+        const uint64_t least = find_least(a, R, E, M.T, n, top, SL, L);
+        kept.least = least > kept.least ? least : kept.least;
         for (int i = tid; i < n; i += NT)
             if (M.T[i] >= kept.least) mine += whole(kept(logit_of(M.T[i]), id_of(M.T[i])), a.weight_bits);
     } else {
@@ -866,7 +903,7 @@ __global__ void __launch_bounds__(NT) k_filter_probs(FilterArgs a, float *probs)
     z.load(a, r, blockIdx.x);
     float *p = probs + (size_t)r * a.V;
     const FilterRow &R = a.s->row[r];
-    const Kept kept{R.least, R.top, a.inv_t, a.min_p};
+    const Kept kept{R.least, R.top, a.inv_t};
     const double inv = 1.0 / ldexp((double)R.total, -a.weight_bits);
     const bool bad = R.bad;
     z.each([&](float x, int j) {
@@ -881,7 +918,7 @@ struct Side { Kept kept; double log_total, inv_total; bool bad; };
 __device__ __forceinline__ Side side_of(const FilterArgs &a, int r) {
     const FilterRow &R = a.s->row[r];
     const double total = ldexp((double)R.total, -a.weight_bits);
-    return Side{Kept{R.least, R.top, a.inv_t, a.min_p}, log(total), 1.0 / total, R.bad != 0};
+    return Side{Kept{R.least, R.top, a.inv_t}, log(total), 1.0 / total, R.bad != 0};
 }
 
 // max(0, p(j) - q(j)), from the logarithms: where the two nearly agree, or all that is left is far below the smallest fp32 number, their
@@ -891,9 +928,9 @@ struct Residual {
     const float *zp, *zq;
     // its logarithm; minus infinity where p does not exceed q
     __device__ __forceinline__ double operator()(int j) const {
-        if (p.kept(zp[j], j) == 0.0) return -INFINITY;
+        if (!p.kept.holds(zp[j], j)) return -INFINITY;
         const double a = ((double)zp[j] - (double)p.kept.top) * p.kept.inv_t - p.log_total;
-        if (q.kept(zq[j], j) == 0.0) return a;
+        if (!q.kept.holds(zq[j], j)) return a;
         const double d = ((double)zq[j] - (double)q.kept.top) * q.kept.inv_t - q.log_total - a;
         return d < 0.0 ? a + log(-expm1(d)) : -INFINITY;
     }
@@ -940,24 +977,29 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             for (int w = 0; w < NW; ++w) c = fmax(c, top_of[w]);
             return c;
         };
-        // the ids that p keeps, one after the other: few, and the arithmetic behind them is long
+        // the ids that p keeps, one after the other: few, and the arithmetic behind them is long (segments beyond the usual length: as they come)
+        const bool usual = a.seg_ids <= kFilterSegIds;
         if (tid == 0) n_kept = 0;
         __syncthreads();
-        auto each_kept = [&](auto f) {                   // (segments beyond the usual length: their ids as they come)
-            if (a.seg_ids <= kFilterSegIds)
-                for (int i = tid; i < n_kept; i += NT) f(ids[i]);
+        if (usual)
+            for (int j = j0 + tid; j < j1; j += NT)
+                if (p.kept.holds(zp[j], j)) ids[atomicAdd(&n_kept, 1)] = j;
+        __syncthreads();
+        const double first = usual && tid < n_kept ? res(ids[tid]) : -INFINITY;
+        double c = first;
+        auto others = [&](auto f) {
+            if (usual)
+                for (int i = tid + NT; i < n_kept; i += NT) f(ids[i]);
             else
                 for (int j = j0 + tid; j < j1; j += NT) f(j);
         };
-        if (a.seg_ids <= kFilterSegIds)
-            for (int j = j0 + tid; j < j1; j += NT)
-                if (!masked(zp[j]) && key_of(zp[j], j) >= p.kept.least) ids[atomicAdd(&n_kept, 1)] = j;
-        __syncthreads();
-        double c = -INFINITY;
-        each_kept([&](int j) { c = fmax(c, res(j)); });
+        others([&](int j) { c = fmax(c, res(j)); });
         c = block_max(c);
         uint64_t sum = 0;
-        if (c > -INFINITY) each_kept([&](int j) { sum += whole(exp(res(j) - c), a.weight_bits); });
+        if (c > -INFINITY) {
+            sum = whole(exp(first - c), a.weight_bits);
+            others([&](int j) { sum += whole(exp(res(j) - c), a.weight_bits); });
+        }
         sum = block_sum(sum, L);
         if (tid == 0) {
             leave(&S.res[2 * blockIdx.x], __builtin_bit_cast(uint64_t, c));
@@ -980,23 +1022,39 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             }
             if (tid == 0) K.hit = -1;
             __syncthreads();
-            // its ids: rounded one by one their weights may add up to a little less than the segment's, whose last id of some weight then stands in
+            // its ids: rounded one by one their weights may add up to a little less than the segment's, whose last id of some weight then stands in.
+            // Those that p keeps first, in their order, so that a thread has one (or a few) of them
             const int s0 = K.seg * a.seg_ids, s1 = min(a.V, s0 + a.seg_ids), per = (a.seg_ids + NT - 1) / NT;
             const int i0 = min(s1, s0 + tid * per), i1 = min(s1, i0 + per);
+            int e0 = i0, e1 = i1;
+            if (usual) {
+                unsigned held = 0;
+                for (int j = i0; j < i1; ++j) held |= p.kept.holds(zp[j], j) ? 1u << (j - i0) : 0;
+                uint64_t all_held;
+                int at = (int)block_scan(__popc(held), L, &all_held);
+                for (int i = 0; i < i1 - i0; ++i)
+                    if (held >> i & 1) ids[at++] = i0 + i;
+                __syncthreads();
+                const int n = (int)all_held, each = (n + NT - 1) / NT;
+                e0 = min(n, tid * each);
+                e1 = min(n, e0 + each);
+            }
+            auto id = [&](int e) { return usual ? ids[e] : e; };
+            const double w_first = e0 < e1 ? exp(res(id(e0)) - total_c) : 0.0;
             uint64_t own = 0;
             int last = -1;
-            for (int j = i0; j < i1; ++j) {
-                const uint64_t y = whole(exp(res(j) - total_c), a.weight_bits);
+            for (int e = e0; e < e1; ++e) {
+                const uint64_t y = whole(e == e0 ? w_first : exp(res(id(e)) - total_c), a.weight_bits);
                 own += y;
-                if (y) last = j;
+                if (y) last = id(e);
             }
             const uint64_t at = K.before + block_scan(own, L, &ignore);
             int hit = -1;
             if (at <= target && target < at + own) {
                 uint64_t s = at;
-                for (int j = i0; j < i1 && hit < 0; ++j) {
-                    s += whole(exp(res(j) - total_c), a.weight_bits);
-                    if (s > target) hit = j;
+                for (int e = e0; e < e1 && hit < 0; ++e) {
+                    s += whole(e == e0 ? w_first : exp(res(id(e)) - total_c), a.weight_bits);
+                    if (s > target) hit = id(e);
                 }
             }
             const int found = (int)block_extreme<true>((uint64_t)(hit + 1), L) - 1;
@@ -1047,6 +1105,7 @@ void filter_finish(FilterArgs &a, float temperature, int top_k, float top_p, flo
     a.top_k = top_k < a.V ? top_k : 0;
     a.top_p = top_p > 0.f && top_p < 1.f ? (double)top_p : 1.0;
     a.min_p = (double)min_p;
+    a.min_x = min_p > 0.f ? (double)temperature * log((double)min_p) : 0.0;
     a.weight_bits = 62;                                  // V weights of up to 2^weight_bits add up to less than 2^63
     for (int v = a.V; v > 0; v >>= 1) --a.weight_bits;
 }

@@ -212,6 +212,34 @@ def test_tokens_that_a_side_does_not_hold(ad):
 
 
 @pytest.mark.parametrize("V", [301, 5000])
+def test_min_p_at_its_edges(ad, V):
+    """Logits next to the border by one step of fp32, a border at the top, at and below the smallest number, and temperatures at which all weights are 1 or all but one 0."""
+    g = model(ad, V)
+    rng = np.random.default_rng(12)
+    z = rng.standard_normal(V).astype(np.float32)
+    z[7] = 5.0
+    for T, mp in [(1.0, 0.05), (0.3, 0.5), (2.5, 1e-4), (1.0, 1.0), (1e30, 1.0), (1e30, 0.5), (1e-30, 1e-3), (1.0, 1e-38), (1e37, 1e-30), (40.0, 0.999999)]:
+        T, mp = filter_plain.f32(T), filter_plain.f32(mp)
+        x = z.copy()
+        with np.errstate(over="ignore"):
+            edge = np.float32(5.0 + T * np.log(mp))
+        if np.isfinite(edge):
+            for i, e in enumerate((edge, np.nextafter(edge, np.float32(9)), np.nextafter(edge, np.float32(-1e38)))):
+                x[20 + i] = min(e, np.float32(5.0))
+        x[30], x[31] = -3.0e38, -0.0
+        print(f"case V={V} T={T} min_p={mp}", flush=True)
+        got = g.ad_filtered_probs(dev(x[None]), ad.Filter(T, 0, 0.0, mp)).cpu().numpy()[0]
+        with np.errstate(over="ignore", under="ignore"):
+            w = np.exp((x.astype(np.float64) - 5.0) / T)
+        # the border to the two last bits of a weight in 64 bits (the exponential's own error)
+        sure, out = w >= mp * (1 + 2.0 ** -51), w < mp * (1 - 2.0 ** -51)
+        assert np.all(got[sure & (w > 2.0 ** -40)] > 0) and np.all(got[out] == 0)
+        tok, prob = g.ad_sample_filtered(dev(x), ad.Filter(T, 0, 0.0, mp), 1 - 2.0 ** -24)
+        assert 0 <= tok < V and not out[tok] and prob > 0
+    g.close()
+
+
+@pytest.mark.parametrize("V", [301, 5000])
 def test_rows_without_a_distribution(ad, V):
     g = model(ad, V)
     rng = np.random.default_rng(9)
