@@ -656,15 +656,11 @@ static int layer_steps(const ad_model *m, ad_kv *kv, int32_t layer, int32_t coun
         }
     };
 
-    // step 2 over an 8-bit cache: rotation and append are a kernel of their own, attention reads every row from the cache
+    // step 2 over an 8-bit cache
     auto attn8 = [&](int32_t ly) {
-        KvqRotate r;
-        r.c = kv->cache8(ly); r.qkv = m->qkv; r.ld = L.nqkv; r.m = n; r.Hq = c.n_q_heads; r.pos0 = pos[0]; r.rope = a.rope;
-        const int e = launch_kvq_rotate(r, ctx);
-        if (e) return e;
         KvqAttn at;
         memset(&at, 0, sizeof at);
-        at.c = r.c; at.q = m->qkv; at.ld_q = L.nqkv; at.m = n; at.Hq = c.n_q_heads;
+        at.c = kv->cache8(ly); at.q = m->qkv; at.ld_q = L.nqkv; at.m = n; at.Hq = c.n_q_heads; at.rope = a.rope; at.pos0 = pos[0];
         for (int i = 0; i < n; ++i) at.see[i] = pos[i];
         at.scale = attn8_scale(L.dh); at.part = kv->part; at.Bo = m->Bo; at.Bo_KT = L.kt_q; at.f16 = ek == kElemF16;
         kvq_attn_finish(at, m->n_wg);

@@ -48,12 +48,6 @@ struct KvqRows {                         // fp32 rows of n tokens at positions p
     int64_t ld;
     int n, pos0;
 };
-struct KvqRotate {                       // a layer step's q, k, v: q is rotated in place, k rotated and stored, v stored
-    KvqCache c;
-    float *qkv;                          // [m][ld]: q heads, k heads, v heads
-    int ld, m, Hq, pos0;
-    const float *rope;                   // rows pos0 .. of the cache's rotary table
-};
 struct KvqExpand {                       // the cache's values in bf16, in the layout of a 16-bit cache of the same stride
     KvqCache c;
     uint16_t *K, *V;
@@ -65,7 +59,11 @@ struct KvqAttn {
     int ld_q;
     int m, Hq, G, R;                     // tokens, query heads, those per kv head, query rows per kv head
     int see[8];                          // last position that token t's queries see
-    int n, n_all;                        // positions that some row sees, that all rows see
+    // a layer step (rope not null): q is the step's q, k, v as they come from their projection, [m][ld_q], the rows' positions are pos0 .. pos0 + m - 1;
+    // queries and keys are rotated, keys and values stored, and attended to
+    const float *rope;                   // rows pos0 .. of the cache's rotary table
+    int pos0;
+    int n, n_all;                        // cached positions (before the call) that some row sees, that all rows see
     int S, per, waves, tiles;            // work items per kv head, blocks of 64 positions and wavefronts per item, tiles of 16 query rows per workgroup
     unsigned mul_S, mul_G, mul_R;
     float scale;                         // of the scores, in powers of two: log2(e) / sqrt(head_dim)
@@ -77,7 +75,6 @@ struct KvqAttn {
 
 int launch_kvq_store(const KvqRows &, const LaunchCtx &);
 int launch_kvq_read(const KvqRows &, const LaunchCtx &);
-int launch_kvq_rotate(const KvqRotate &, const LaunchCtx &);
 int launch_kvq_expand(const KvqExpand &, const LaunchCtx &);
 // fills in what follows from the other fields (G, R, n, n_all, S, per, multipliers), for a grid of n_wg compute units
 void kvq_attn_finish(KvqAttn &, int n_wg);
