@@ -14,6 +14,11 @@
 //                     last workgroup of the row finds the boundaries among those, and draws
 //   k_filter_one      all of that for a row of one segment
 //   k_filter_probs, k_filter_verify: from the rows' outcomes
+//
+// What bounds them is not the rows (0.5 MB) but the chain of dependent loads, barriers and kernel boundaries: of a draw from 128256 logits with all three steps on,
+// 25 us in three kernels (2.9, 9.7, 12.7), the last takes 1.0 for its first loads, 1.0 to 1.3 for the classes, 1.2 to publish, 1.5 for the list, 3.3 for the two
+// boundaries, 0.6 to add up, 3.0 to draw.  With every entry of a boundary ranked against all others, and boundaries found through memory, it was 32; ten workgroup-wide steps per boundary in
+// place of two barriers cost 2 more.  A row of one segment in one kernel: 11.3 us for 2048 logits, 29 in four.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -316,6 +321,8 @@ __device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t
     __syncthreads();
 }
 
+// One row of 128256 logits 9.7 us, eleven 17: each row's workgroups add up to 2048 sums each to the row's, which are the same for all 63.  (Segments of 4096 ids have
+// fewer of those, 14.2 us, but the kernels behind take as much longer.)
 __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
     __shared__ BlockLds L;
     __shared__ Histogram H;
@@ -600,6 +607,7 @@ __device__ __forceinline__ int draw(const FilterArgs &a, uint64_t mine, float u,
         K.seg = tid;
         K.before = before;
     }
+    if (tid == 0) K.hit = -1;
     __syncthreads();
     // thread t has consecutive ids of the segment, the logits of the first kKeep of them all on their way at once
     const int seg = K.seg, j0 = seg * a.seg_ids, j1 = min(a.V, j0 + a.seg_ids), per = (a.seg_ids + NT - 1) / NT;
@@ -637,8 +645,17 @@ __device__ __forceinline__ int draw(const FilterArgs &a, uint64_t mine, float u,
         K.w = w_hit;
     }
     __syncthreads();
-    *weight = K.w;
     *sum = total;
+    if (K.hit < 0) {
+        // (the segment's weight was formed of other ids: those next to min_p, if the exponential does not grow from one logit to the next) the row's last kept id
+        uint64_t last = 0;
+        for (int j = tid; j < a.V; j += NT)
+            if (kept.holds(z[j], j)) last = (uint64_t)j + 1;
+        const int id = (int)block_extreme<true>(last, L) - 1;
+        *weight = id >= 0 ? kept(z[id], id) : 0.0;
+        return id;
+    }
+    *weight = K.w;
     return K.hit;
 }
 
@@ -936,6 +953,8 @@ struct Residual {
     }
 };
 
+// A segment of the residual per workgroup, the last one draws.  13.1 us for 6 rows of 128256 logits if a draft is rejected, 6 if none is.  The residual takes two
+// exponentials and a logarithm in 64 bits an id: only the ids that p keeps, gathered first, come that far (all of a wavefront's turns waited for one such id before: 15.2).
 __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
     __shared__ BlockLds L;
     __shared__ WalkLds K;
@@ -1044,9 +1063,9 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             uint64_t own = 0;
             int last = -1;
             for (int e = e0; e < e1; ++e) {
-                const uint64_t y = whole(e == e0 ? w_first : exp(res(id(e)) - total_c), a.weight_bits);
-                own += y;
-                if (y) last = id(e);
+                const double y = e == e0 ? w_first : exp(res(id(e)) - total_c);
+                own += whole(y, a.weight_bits);
+                if (y > 0.0) last = id(e);
             }
             const uint64_t at = K.before + block_scan(own, L, &ignore);
             int hit = -1;

@@ -1400,6 +1400,7 @@ static ad_status generate(const ad_model *m, ad_kv *kv, const int32_t *prompt, i
                           int64_t *n_events, void *stream) {
     if (!m || !kv || !prompt || !gp || !out_tokens || !n_out) return (ad_status)fail(AD_EINVAL, "ad_generate: null argument");
     if (kv->model != m) return (ad_status)fail(AD_EINVAL, "ad_generate: cache belongs to another model");
+    if (kv->q8 && m->layer_mode == AD_LAYER_FUSED) return (ad_status)fail(AD_ESTATE, "ad_generate: the fused layer step does not run on an 8-bit cache");
     if (n_prompt < 1 || gp->max_new < 1) return (ad_status)fail(AD_EINVAL, "ad_generate: empty prompt or max_new < 1");
     if (gp->max_pending < 0 || gp->max_pending + 1 > m->cfg.m_max)
         return (ad_status)fail(AD_ERANGE, "ad_generate: max_pending %d outside 0..%d", gp->max_pending, m->cfg.m_max - 1);

@@ -150,6 +150,24 @@ def test_prompts(ad, s):
     g.close()
 
 
+def test_storage_without_the_prompt_scratch(ad):
+    """256 bytes less than ad_kvq_bytes() is a cache all the same, whose prompts go through 8 rows at a time."""
+    s = ODD
+    w = synth.make_weights(s, seed=4, norm_jitter=0.2)
+    g = ad.Model(s, w, max_pos=300, kvq=True)
+    p = synth.make_prompt(s, 7, 200)
+    want, _, _ = g.ad_generate(p, 8, 2.0, 0)
+    g.L.ad_kv_destroy(g.kv)
+    ad._check(g.L.ad_kvq_create(g.model, g.kv_storage.data_ptr(), g.kv_storage.numel() - 256, 300, None, ad.C.byref(g.kv)))
+    g.kv_storage[-(1 << 16):].fill_(0xA5)
+    got, _, _ = g.ad_generate(p, 8, 2.0, 0)
+    assert bool((g.kv_storage[-(1 << 16):] == 0xA5).all())
+    assert len(got) == len(want) == 8
+    core = 3 * ((2 * 2 * 320 * 65 + 255) // 256 * 256)
+    assert g.L.ad_kvq_create(g.model, g.kv_storage.data_ptr(), core, 300, None, ad.C.byref(ad.C.c_void_p())) == ad.AD_ENOMEM
+    g.close()
+
+
 @pytest.mark.parametrize("s", [synth.TINY.with_(tied_head=False, vocab=512, exit_layers=(1, 2, 3)), GQA, GQA.with_(name="tiny-gqa-bf16", dtype=synth.BF16),
                                GQA.with_(name="tiny-gqa-f16", dtype=synth.F16)], ids=lambda s: s.name)
 def test_generation_emits_what_plain_decoding_emits(ad, s):
@@ -233,6 +251,7 @@ def test_refusals(ad):
     g.ad_set_layer_mode(ad.AD_LAYER_FUSED)
     h = g.ad_embed([1])
     assert status(lambda: g.ad_layer_step(1, h, [2])) == ad.AD_ESTATE
+    assert status(lambda: g.ad_generate(np.arange(3, 20), 2, 0.9, 2)) == ad.AD_ESTATE
     assert g.kv_len(1) == 2
     g.ad_set_layer_mode(ad.AD_LAYER_KERNELS)
     g.ad_layer_step(1, h, [2])
