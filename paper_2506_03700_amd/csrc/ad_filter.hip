@@ -303,26 +303,25 @@ __device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t
     if (a.top_p < 1.0) {
         // top-p: its share of what top-k keeps, which is known up to that bucket's weight; the buckets that it may end in
         // (a factor for the roundings of these sums to doubles: more buckets than need be do no harm)
-        const double lo = a.top_p * (double)(R.bk >= 0 ? R.weight_k : all_w) * (1.0 - 1e-12);
-        const double hi = a.top_p * (double)(R.bk >= 0 ? R.weight_k + in_k : all_w) * (1.0 + 1e-12);
+        const uint64_t lo = (uint64_t)(a.top_p * (double)(R.bk >= 0 ? R.weight_k : all_w) * (1.0 - 1e-12));
+        const uint64_t hi = (uint64_t)(a.top_p * (double)(R.bk >= 0 ? R.weight_k + in_k : all_w) * (1.0 + 1e-12)) + 1;
         uint64_t wb = w0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             // the first bucket that reaches lo, the last that starts at or before hi (the buckets in between may be empty)
-            const bool before = (double)(wb + w[i]) < lo, behind = (double)wb > hi;
-            if (!before && ((double)wb < lo || tid * PER + i == 0)) {
+            if (wb + w[i] >= lo && (wb < lo || tid * PER + i == 0)) {
                 R.p0 = tid * PER + i;
                 R.weight_p = wb;
             }
-            if (!behind && (double)(wb + w[i]) > hi) R.p1 = tid * PER + i;
+            if (wb <= hi && (wb + w[i] > hi || tid * PER + i == kFilterBuckets - 1)) R.p1 = tid * PER + i;
             wb += w[i];
         }
     }
     __syncthreads();
 }
 
-// One row of 128256 logits 9.7 us, eleven 17: each row's workgroups add up to 2048 sums each to the row's, which are the same for all 63.  (Segments of 4096 ids have
-// fewer of those, 14.2 us, but the kernels behind take as much longer.)
+// One row of 128256 logits 9.7 us.  Each of a row's workgroups adds up to 2048 sums to the row's, the same ones for all: with several rows that is what takes longest, so
+// that workgroups beyond one per compute unit take several segments each (eleven rows WAS 17 us).
 __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
     __shared__ BlockLds L;
     __shared__ Histogram H;
@@ -335,13 +334,16 @@ __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
     bool bad;
     const float top = row_top(a, r, &bad);
     __syncthreads();
-    if (!bad) z.each([&](float x, int) { H.add(a, x, top); });
+    for (int seg = blockIdx.x; seg < a.n_seg && !bad; seg += gridDim.x) {
+        if (seg != (int)blockIdx.x) z.load(a, r, seg);
+        z.each([&](float x, int) { H.add(a, x, top); });
+    }
     __syncthreads();
     for (int b = tid; b < kFilterBuckets; b += NT) {
         if (a.top_k && H.count[b]) atomicAdd(&S.count[r][b], H.count[b]);
         if (a.top_p < 1.0 && H.weight[b]) atomicAdd((unsigned long long *)&S.weight[r][b], (unsigned long long)H.weight[b]);
     }
-    if (!last_of(S.arrivals[r], a.n_seg, L)) return;
+    if (!last_of(S.arrivals[r], gridDim.x, L)) return;
     constexpr int PER = kFilterBuckets / NT;
     uint64_t w[PER];
     uint32_t c[PER];
@@ -1106,7 +1108,9 @@ int launch_rows(const FilterArgs &a, const LaunchCtx &c, float *probs = nullptr)
     int rc = launch<k_filter_top>(c, grid, wg, 0, a);
     if (rc) return rc;
     if (a.top_k || a.top_p < 1.0) {
-        if ((rc = launch<k_filter_buckets>(c, grid, wg, 0, a))) return rc;
+        // (at least one workgroup a row)
+        const int most = c.n_wg / a.rows > 1 ? c.n_wg / a.rows : 1;
+        if ((rc = launch<k_filter_buckets>(c, dim3(a.n_seg < most ? a.n_seg : most, a.rows), wg, 0, a))) return rc;
         return launch<k_filter_row<true>>(c, grid, wg, 0, a);
     }
     return launch<k_filter_row<false>>(c, grid, wg, 0, a);
