@@ -13,6 +13,8 @@ constexpr int kFilterMaxSegs = kFilterThreads;
 constexpr int kFilterBuckets = 2048;                 // of logits, by their distance from the row's largest
 constexpr int kFilterRows = 15;                      // 8 final and 7 draft rows of a verification
 constexpr int kFilterList = 4096;                    // ids of the buckets that a boundary lies in, that a row's list has places for
+constexpr int kFilterFew = 128;                      // largest top-k that a single kernel takes,
+constexpr int kFilterFewList = 8192;                 // if a list of this many has places for that many ids of each segment
 
 // What the kernels leave one another, for one row.
 struct FilterRow {
@@ -33,7 +35,7 @@ struct FilterScratch {                               // dev; histograms and arri
     uint32_t count[kFilterRows][kFilterBuckets];
     float seg_top[kFilterRows][kFilterMaxSegs];
     uint64_t seg_weight[kFilterRows][kFilterMaxSegs];
-    uint64_t list[kFilterRows][kFilterList];         // per segment: logit's bits, id
+    uint64_t list[kFilterRows][kFilterFewList];      // per segment: logit's bits, id
     uint32_t arrivals[kFilterRows + 1][32];
     FilterRow row[kFilterRows];
     uint64_t res[2 * kFilterMaxSegs];                // residual, per segment: the bits of the logarithm of its largest weight, its weight

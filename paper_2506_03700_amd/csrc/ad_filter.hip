@@ -13,12 +13,14 @@
 //   k_filter_row      weight of each segment's ids that are kept for certain, and a list of the ids in the boundaries' buckets; the
 //                     last workgroup of the row finds the boundaries among those, and draws
 //   k_filter_one      all of that for a row of one segment
+//   k_filter_few      all of that for a small top-k: the first top_k ids of the row are among the first top_k of its segments
 //   k_filter_probs, k_filter_verify: from the rows' outcomes
 //
 // What bounds them is not the rows (0.5 MB) but the chain of dependent loads, barriers and kernel boundaries: of a draw from 128256 logits with all three steps on,
-// 25 us in three kernels (2.9, 9.7, 12.7), the last takes 1.0 for its first loads, 1.0 to 1.3 for the classes, 1.2 to publish, 1.5 for the list, 3.3 for the two
+// 24 us in three kernels (2.9, 9.7, 12.0), the last takes 1.0 for its first loads, 1.0 to 1.3 for the classes, 1.2 to publish, 1.5 for the list, 3.3 for the two
 // boundaries, 0.6 to add up, 3.0 to draw.  With every entry of a boundary ranked against all others, and boundaries found through memory, it was 32; ten workgroup-wide steps per boundary in
-// place of two barriers cost 2 more.  A row of one segment in one kernel: 11.3 us for 2048 logits, 29 in four.
+// place of two barriers cost 2 more.  A small top-k in one kernel: 12.7 (largest 50).  A row of one segment in
+// one kernel: 11.3 us for 2048 logits, 29 in four.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -220,16 +222,18 @@ __global__ void __launch_bounds__(NT) k_filter_top(FilterArgs a) {
 }
 
 // of the row, to every thread (every wavefront looks at all segments, which saves the barriers); *bad: it has no distribution
+// PUBLISHED: by other workgroups of this launch
+template <bool PUBLISHED = false>
 __device__ __forceinline__ float row_top(const FilterArgs &a, int r, bool *bad) {
     constexpr int PER = kFilterMaxSegs / 64;
     const int lane = threadIdx.x & 63;
-    const float *seg = a.s->seg_top[r];
-    float m = lane < a.n_seg ? seg[lane] : -INFINITY;
+    auto at = [&](int i) { return PUBLISHED ? __hip_atomic_load(&a.s->seg_top[r][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : a.s->seg_top[r][i]; };
+    float m = lane < a.n_seg ? at(lane) : -INFINITY;
     bool nan = m != m;
     if (a.n_seg > 64) {
         float v[PER - 1];
 #pragma unroll
-        for (int i = 1; i < PER; ++i) v[i - 1] = lane + 64 * i < a.n_seg ? seg[lane + 64 * i] : -INFINITY;
+        for (int i = 1; i < PER; ++i) v[i - 1] = lane + 64 * i < a.n_seg ? at(lane + 64 * i) : -INFINITY;
 #pragma unroll
         for (int i = 1; i < PER; ++i) {
             nan |= v[i - 1] != v[i - 1];
@@ -321,7 +325,7 @@ __device__ __forceinline__ void find_buckets(const FilterArgs &a, const uint64_t
 }
 
 // One row of 128256 logits 9.7 us.  Each of a row's workgroups adds up to 2048 sums to the row's, the same ones for all: with several rows that is what takes longest, so
-// that workgroups beyond one per compute unit take several segments each (eleven rows WAS 17 us).
+// that workgroups beyond one per compute unit take several segments each (eleven rows 17 -> 13.3 us).
 __global__ void __launch_bounds__(NT) k_filter_buckets(FilterArgs a) {
     __shared__ BlockLds L;
     __shared__ Histogram H;
@@ -914,6 +918,176 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
 }
 
 // ---------------------------------------------------------------------------------------------------
+// a small top-k
+// ---------------------------------------------------------------------------------------------------
+// The smallest key of the first k of the entries that `each` goes through (a callable given the logit and id of each entry of this thread), 0 if there are no more than
+// k; top: their largest logit.  By buckets, of which the last is ranked; one of more than kRank entries is cut by key until it is short enough.
+template <class Each>
+__device__ __forceinline__ uint64_t first_k(const FilterArgs &a, Each each, float top, uint32_t k, uint32_t *count, SelectLds &S, BlockLds &L) {
+    constexpr int PER = kFilterBuckets / NT;
+    const int tid = threadIdx.x, lane = tid & 63;
+    __syncthreads();
+    for (int b = tid; b < kFilterBuckets; b += NT) count[b] = 0;
+    if (tid == 0) S.n = 0;
+    __syncthreads();
+    each([&](float x, int) {
+        if (!masked(x)) atomicAdd(&count[bucket_of(x, top, a.bucket_scale)], 1u);
+    });
+    __syncthreads();
+    uint32_t c[PER];
+    uint64_t sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        c[i] = count[tid * PER + i];
+        sum += c[i];
+    }
+    uint64_t at = block_scan(sum, L, &all);
+    if (all <= k) return 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (at < k && at + c[i] >= k) {
+            S.bin = tid * PER + i;
+            S.before = at;
+        }
+        at += c[i];
+    }
+    __syncthreads();
+    const int bucket = S.bin;
+    uint32_t left = k - (uint32_t)S.before;                  // of the bucket's entries, 1 at least
+    uint64_t n = count[bucket], lo = 0, hi = ~0ull;
+    auto inside = [&](float x, uint64_t key) { return !masked(x) && bucket_of(x, top, a.bucket_scale) == bucket && key >= lo && key <= hi; };
+    if (n > kRank) {
+        uint64_t kl = ~0ull, kh = 0;
+        each([&](float x, int id) {
+            const uint64_t key = key_of(x, id);
+            if (!inside(x, key)) return;
+            kl = key < kl ? key : kl;
+            kh = key > kh ? key : kh;
+        });
+        lo = block_extreme<false>(kl, L);
+        hi = block_extreme<true>(kh, L);
+        while (n > kRank) {
+            const int shift = 64 - __clzll((long long)((hi - lo) / NT));         // (hi - lo) >> shift < NT
+            __syncthreads();
+            S.c[tid] = 0;
+            __syncthreads();
+            each([&](float x, int id) {
+                const uint64_t key = key_of(x, id);
+                if (inside(x, key)) atomicAdd(&S.c[(hi - key) >> shift], 1u);
+            });
+            __syncthreads();
+            const uint64_t before = block_scan(S.c[tid], L, &all);
+            if (before < left && before + S.c[tid] >= left) {
+                S.bin = tid;
+                S.before = before;
+            }
+            __syncthreads();
+            const uint64_t new_hi = hi - ((uint64_t)S.bin << shift), span = ((uint64_t)1 << shift) - 1;
+            left -= (uint32_t)S.before;
+            n = S.c[S.bin];
+            lo = new_hi - lo > span ? new_hi - span : lo;
+            hi = new_hi;
+        }
+    }
+    each([&](float x, int id) {
+        const uint64_t key = key_of(x, id);
+        if (inside(x, key)) S.key[atomicAdd(&S.n, 1)] = key;
+    });
+    __syncthreads();
+    // every wavefront ranks them for itself
+    const uint64_t mine = lane < (int)n ? S.key[lane] : 0;
+    uint32_t rank = 0;
+    for (int i = 0; i < (int)n; ++i) rank += S.key[i] > mine;
+    return lane_u64(mine, __ffsll(__ballot(lane < (int)n && rank == left - 1)) - 1);
+}
+
+// Every workgroup lists its segment's first top_k; the row's last one finds the row's among those and takes the other steps and the draw on what is left, an id a thread.
+// PER: of the list's places, to a thread.
+template <int PER>
+__global__ void __launch_bounds__(NT) k_filter_few(FilterArgs a) {
+    __shared__ BlockLds L;
+    __shared__ SelectLds SL;
+    __shared__ uint32_t count[kFilterBuckets];
+    __shared__ uint64_t T[NT];
+    __shared__ uint64_t key[kFilterFew], weight[kFilterFew];
+    __shared__ int n_listed;
+    const int r = blockIdx.y, tid = threadIdx.x;
+    FilterScratch &S = *a.s;
+    SegLogits z;
+    z.load(a, r, blockIdx.x);
+    const float seg_top = z.top(L);
+    if (tid == 0) n_listed = 0;
+    if (fabsf(seg_top) < INFINITY) {
+        const uint64_t least = first_k(a, [&](auto f) { z.each(f); }, seg_top, (uint32_t)a.top_k, count, SL, L);
+        z.each([&](float x, int j) {
+            if (!masked(x) && key_of(x, j) >= least) T[atomicAdd(&n_listed, 1)] = (uint64_t)__float_as_uint(x) << 32 | (uint32_t)j;
+        });
+    }
+    __syncthreads();
+    if (tid < a.places) leave(&S.list[r][blockIdx.x * a.places + tid], tid < n_listed ? T[tid] : kUnused);
+    if (tid == 0) leave(&S.seg_top[r][blockIdx.x], seg_top);
+    if (!last_of(S.arrivals[r], a.n_seg, L)) return;
+
+    // (every place of the list is on its way before the first is looked at)
+    uint64_t e[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) e[i] = tid + i * NT < a.n_seg * a.places ? seen(&S.list[r][tid + i * NT]) : kUnused;
+    bool bad;
+    const float top = row_top<true>(a, r, &bad);
+    if (bad) {
+        no_distribution(a, r, top);
+        return;
+    }
+    auto listed = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (e[i] != kUnused) f(__uint_as_float((uint32_t)(e[i] >> 32)), (int)(uint32_t)e[i]);
+    };
+    const uint64_t least_k = first_k(a, listed, top, (uint32_t)a.top_k, count, SL, L);
+    if (tid == 0) n_listed = 0;
+    __syncthreads();
+    listed([&](float x, int id) {
+        const uint64_t k = key_of(x, id);
+        if (k >= least_k) key[atomicAdd(&n_listed, 1)] = k;
+    });
+    __syncthreads();
+    const int n = n_listed;                                  // top_k, or fewer
+    const uint64_t mine = tid < n ? key[tid] : 0;
+    const double w = tid < n ? weight_of(logit_of(mine), top, a.inv_t) : 0.0;
+    if (tid < n) weight[tid] = whole(w, a.weight_bits);
+    T[tid] = 0;
+    __syncthreads();
+    // kept: less than top_p of the weight of all before it, and at least min_p of the largest
+    bool keep = tid < n && w >= a.min_p;
+    if (a.top_p < 1.0 && tid < n) {
+        uint64_t before = 0, all = 0;
+        for (int i = 0; i < n; ++i) {
+            before += key[i] > mine ? weight[i] : 0;
+            all += weight[i];
+        }
+        keep = keep && before < (uint64_t)ceil(a.top_p * (double)all);
+    }
+    __syncthreads();
+    if (tid < n && !keep) weight[tid] = 0;
+    if (!a.tok_out) {
+        if (keep) atomicAdd((unsigned long long *)&T[id_of(mine) / a.seg_ids], (unsigned long long)weight[tid]);
+        const uint64_t least = block_extreme<false>(keep ? mine : ~0ull, L);     // (its barriers: the segments' weights are complete)
+        (void)outcome(a, r, top, least, T[tid], L);
+        return;
+    }
+    __syncthreads();
+    if (tid >= n) return;
+    uint64_t total = 0, ahead = 0;
+    for (int i = 0; i < n; ++i) {
+        total += weight[i];
+        ahead += id_of(key[i]) < id_of(mine) ? weight[i] : 0;
+    }
+    uint64_t target = (uint64_t)((double)a.u * (double)total);
+    target = target < total ? target : total - 1;
+    if (ahead <= target && target < ahead + weight[tid]) report_draw(a, id_of(mine), (float)(w / ldexp((double)total, -a.weight_bits)));
+}
+
+// ---------------------------------------------------------------------------------------------------
 // the distributions
 // ---------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(NT) k_filter_probs(FilterArgs a, float *probs) {
@@ -1105,6 +1279,15 @@ int launch_rows(const FilterArgs &a, const LaunchCtx &c, float *probs = nullptr)
     if (a.V < 1 || a.rows < 1 || a.rows > kFilterRows || a.n_seg > kFilterMaxSegs || !(a.inv_t > 0.0)) return (int)hipErrorInvalidValue;
     const dim3 grid(a.n_seg, a.rows), wg(NT);
     if (a.n_seg == 1) return launch<k_filter_one>(c, dim3(a.rows), wg, 0, a, probs);
+    // A small top-k takes one kernel and not three: a draw from 32016 logits by the largest 128 of them takes 14.4 us where one by the largest 129 takes 22.7,
+    // 8 rows' distributions of 128256 by the largest 50 take 17.9 and by 129 31.0.  The list of fewer places has a shorter program (top-k 50 of
+    // 128256: 12.7 us, and 14.1 with 16 places to a thread); kept in LDS, it leaves a compute unit room for one workgroup (8 rows 27.6).
+    if (a.top_k && a.top_k <= kFilterFew && a.top_k * a.n_seg <= kFilterFewList) {
+        FilterArgs few = a;
+        few.places = a.top_k;
+        constexpr int PER = kFilterFewList / NT;
+        return a.top_k * a.n_seg <= kFilterFewList / 2 ? launch<k_filter_few<PER / 2>>(c, grid, wg, 0, few) : launch<k_filter_few<PER>>(c, grid, wg, 0, few);
+    }
     int rc = launch<k_filter_top>(c, grid, wg, 0, a);
     if (rc) return rc;
     if (a.top_k || a.top_p < 1.0) {

@@ -265,13 +265,42 @@ def test_rows_without_a_distribution(ad, V):
     g.close()
 
 
-def test_repeated_and_captured(ad):
+@pytest.mark.parametrize("V", [2049, 32016, 128256, 200001])
+def test_a_small_top_k(ad, V):
+    """As many ids as one kernel takes and one more, at rows where they all lie in one segment, in all of them, or are equal."""
+    rng = np.random.default_rng(V + 3)
+    g = model(ad, V)
+    for k in (1, 64, 65, 128, 129):
+        for kind in ("one segment", "every segment", "flat", "steps", "close", "few left", "tail"):
+            z = logits(rng, V, kind if kind in ("flat", "steps", "close") else "tail")
+            if kind == "one segment":
+                z[-min(V - 2048, 200):] += np.float32(20)
+            elif kind == "every segment":
+                z[::max(1, V // k)] = 15
+            elif kind == "few left":
+                z[rng.permutation(V)[max(1, k - 2):]] = -np.inf
+            for p, mp in ((0.0, 0.0), (0.8, 0.0), (0.9, 0.3)):
+                print(f"case V={V} {kind} top_k={k} top_p={p} min_p={mp}", flush=True)
+                f = (0.9, k, p, mp)
+                got = g.ad_filtered_probs(dev(z[None]), ad.Filter(*f)).cpu().numpy()[0]
+                check_probs(got.astype(np.float64), z, f, kind)
+                want = Row(z, *f)
+                for u in (0.0, filter_plain.f32(rng.random()), 1 - 2.0 ** -24):
+                    tok, prob = g.ad_sample_filtered(dev(z), ad.Filter(*f), u)
+                    t, margin = filter_plain.draw(want.p, u)
+                    assert tok == t or min(margin, want.margin) < MARGIN
+                    assert want.margin < MARGIN or abs(prob - want.p[tok]) <= (2.0 ** -24 + MARGIN) * want.p[tok]
+    g.close()
+
+
+@pytest.mark.parametrize("f", [(0.9, 300, 0.93, 0.001), (0.9, 40, 0.93, 0.001), (0.9, 0, 0.0, 0.0)], ids=["boundaries", "small-top-k", "off"])
+def test_repeated_and_captured(ad, f):
     """Same bits again, from another stream, and in graphs that are replayed over new rows with eager calls in between."""
     import torch
     V, m = 32016, 4
     g = model(ad, V)
     rng = np.random.default_rng(11)
-    f = ad.Filter(0.9, 300, 0.93, 0.001)
+    f = ad.Filter(*f)
     rows = [dev(np.stack([logits(rng, V, "tail") for _ in range(2 * m - 1)])) for _ in range(4)]
     draft = np.array([int(rows[0][m + k].argmax()) for k in range(m - 1)], dtype=np.int32)
     ua, ur = np.full(m - 1, 0.6, np.float32), np.full(m - 1, 0.3, np.float32)
