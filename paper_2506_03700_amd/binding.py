@@ -300,9 +300,12 @@ class Model:
         torch = self.torch
         if self.kvq:
             had = self.kv_len(layer)
-            self.kv_set_len(layer, 0)
-            self.ad_kvq_append(layer, *(torch.as_tensor(x).to(self.device, torch.float32).contiguous() for x in (k, v)), 0)
-            self.kv_set_len(layer, had)
+            try:
+                self.kv_set_len(layer, 0)
+                if k.shape[0]:
+                    self.ad_kvq_append(layer, *(torch.as_tensor(x).to(self.device, torch.float32).contiguous() for x in (k, v)), 0)
+            finally:
+                self.kv_set_len(layer, had)
             return
         K, V = self.kv_views()
         n = k.shape[0]
@@ -312,6 +315,8 @@ class Model:
     def kv_read(self, layer: int, n: int):
         """Positions [0, n) of one layer as float64 numpy arrays [n, kv heads, head_dim]."""
         if self.kvq:
+            if n == 0:
+                return tuple(np.empty((0, self.shape.n_kv_heads, self.shape.head_dim)) for _ in "kv")
             return tuple(x.cpu().numpy().astype(np.float64) for x in self.ad_kvq_read(layer, 0, n))
         K, V = self.kv_views()
         k = K[layer - 1, :, :n, :].float().permute(1, 0, 2).cpu().numpy().astype(np.float64)
@@ -442,7 +447,7 @@ class Model:
     def ad_filtered_probs(self, logits, flt: Filter):
         """The filtered distributions of rows of logits, float32 [m, vocab]."""
         torch = self.torch
-        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.dim() == 2 and logits.shape[1] == self.shape.vocab
+        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.device == self.device and logits.dim() == 2 and logits.shape[1] == self.shape.vocab
         p = torch.empty_like(logits)
         _check(self.L.ad_filtered_probs(self.model, logits.data_ptr(), logits.shape[0], C.byref(flt), p.data_ptr(), _stream_ptr(torch)))
         return p
@@ -450,7 +455,7 @@ class Model:
     def ad_sample_filtered(self, logits, flt: Filter, u: float):
         """(token, its probability) drawn from the filtered distribution with the uniform draw u."""
         torch = self.torch
-        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.numel() == self.shape.vocab
+        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.device == self.device and logits.numel() == self.shape.vocab
         tok, prob = C.c_int32(), C.c_float()
         _check(self.L.ad_sample_filtered_wait(self.model, logits.data_ptr(), C.byref(flt), u, C.byref(tok), C.byref(prob), _stream_ptr(torch)))
         return tok.value, prob.value
@@ -459,13 +464,14 @@ class Model:
         """Eq. 2 between filtered distributions: (n_accept, next_token, ratios[m-1])."""
         torch = self.torch
         m, V = final_logits.shape
-        assert final_logits.dtype == torch.float32 and final_logits.is_contiguous() and V == self.shape.vocab
+        assert final_logits.dtype == torch.float32 and final_logits.is_contiguous() and final_logits.device == self.device and V == self.shape.vocab
         d = np.ascontiguousarray(draft, dtype=np.int32)
         ua = np.ascontiguousarray(u_accept, dtype=np.float32)
         ur = np.ascontiguousarray(u_resample, dtype=np.float32)
         assert d.size == ua.size == ur.size == m - 1
         if m > 1:
-            assert draft_logits.dtype == torch.float32 and draft_logits.is_contiguous() and tuple(draft_logits.shape) == (m - 1, V)
+            assert draft_logits.dtype == torch.float32 and draft_logits.is_contiguous() and draft_logits.device == self.device
+            assert tuple(draft_logits.shape) == (m - 1, V)
         n, nxt, ratio = C.c_int32(), C.c_int32(), np.empty(m - 1, dtype=np.float32)
         at = lambda a: a.ctypes.data if m > 1 else None
         _check(self.L.ad_verify_filtered_wait(self.model, final_logits.data_ptr(), draft_logits.data_ptr() if m > 1 else None, at(d), m, C.byref(flt),

@@ -366,6 +366,10 @@ def test_refusals(ad):
         assert status(lambda: g.ad_verify_filtered(z, z[:1], [1], f, [0.5], [0.5], u)) == ad.AD_ERANGE
     assert status(lambda: g.ad_verify_filtered(z, z[:1], [301], f, [0.5], [0.5], 0.5)) == ad.AD_ERANGE
     assert status(lambda: g.ad_verify_filtered(z, z[:1], [-1], f, [0.5], [0.5], 0.5)) == ad.AD_ERANGE
+    for call in (lambda: g.ad_filtered_probs(z.cpu(), f), lambda: g.ad_sample_filtered(z[0].cpu(), f, 0.5),
+                 lambda: g.ad_verify_filtered(z, z[:1].cpu(), [1], f, [0.5], [0.5], 0.5), lambda: g.ad_filtered_probs(z.double(), f)):
+        with pytest.raises(AssertionError):                          # (host memory, another type)
+            call()
     nine = torch.zeros((9, 301), device="cuda:0")
     assert status(lambda: g.ad_filtered_probs(nine, f)) == ad.AD_ERANGE
     assert status(lambda: g.ad_verify_filtered(nine, nine[:8], [1] * 8, f, [0.5] * 8, [0.5] * 8, 0.5)) == ad.AD_ERANGE
@@ -436,4 +440,41 @@ def test_generation(ad, dtype, kvq):
     with pytest.raises(ad.AdError) as e:
         g.ad_generate(p, n_new, 0.0, 5, top_k=4)                     # a filter is for sampled decoding
     assert e.value.status == ad.AD_ERANGE
+    g.close()
+
+
+@pytest.mark.parametrize("f", [dict(top_k=12, min_p=0.01), dict(top_k=200, top_p=0.9), dict(min_p=0.05)], ids=str)
+def test_generation_with_longer_rows(ad, f):
+    """A vocabulary of several segments and an 8-bit cache: plain runs draw from the filtered final distribution, runs with early exits emit what it holds, whatever is
+    issued ahead."""
+    s = UNTIED.with_(dtype=synth.BF16, vocab=5000)
+    max_pos, n_new, T, near = 96, 24, 0.05, 0.2
+    g = ad.Model(s, synth.make_weights(s, seed=0, with_T=True, T_std=0.03), max_pos, kvq=True)
+    p = synth.make_prompt(s, 0, 40)
+    u = synth.make_uniforms(s, 3, max_pos)
+    n = exact = 0
+    for gamma, cap in ((2.0, 0), (0.0, 6)):
+        toks, _, _ = g.ad_generate(p, n_new, gamma, cap, temperature=T, uniforms=u, **f)
+        again, _, _ = g.ad_generate(p, n_new, gamma, cap, temperature=T, uniforms=u, no_issue_ahead=True, **f)
+        assert np.array_equal(toks, again) and len(toks) == n_new
+        seq = np.concatenate([p, toks[:-1]])
+        g.kv_truncate(0)
+        for i in range(0, len(seq), 8):
+            h = g.ad_embed(seq[i:i + 8])
+            g.ad_layer_steps(1, s.n_layers, h, i + np.arange(len(seq[i:i + 8])))
+            for j, z in enumerate(g.ad_head_logits(s.n_layers, h).cpu().numpy()):
+                at = i + j - (len(p) - 1)
+                if at < 0:
+                    continue
+                row = Row(z, T, f.get("top_k", 0), f.get("top_p", 0.0), f.get("min_p", 0.0))
+                want, margin = filter_plain.draw(row.p, u[i + j, len(s.exit_layers)])
+                # (logits of another grouping of the rows: a draw or an edge this near may fall to the other side)
+                edge = np.sort(z)[-f["top_k"]] if "top_k" in f else np.inf
+                assert row.p[toks[at]] > 0 or row.margin < near or abs(float(z[toks[at]]) - edge) < near * T
+                if cap == 0:
+                    n += 1
+                    exact += toks[at] == want
+                    assert toks[at] == want or min(margin, row.margin) < near
+    # logits are off by some 2^-9, weights by 2^-9 / T = 0.04 of themselves: so is a sum of weights, and about as many draws
+    assert exact >= 0.85 * n and n == n_new
     g.close()

@@ -98,6 +98,24 @@ def test_entries_that_are_no_numbers(ad):
     g.close()
 
 
+def test_filling_and_reading_a_layer(ad):
+    """kv_fill and kv_read, as for any cache: lengths stay, no rows are no error, a refusal changes nothing."""
+    g = model(ad, (4, 2, 64), 70)
+    k, v = rows(np.random.default_rng(2), 70, 2, 64)
+    g.kv_set_len(1, 70)
+    g.kv_fill(1, k, v)
+    g.kv_fill(1, k[:0], v[:0])
+    assert g.kv_len(1) == 70 and g.kv_len(2) == 0
+    with np.errstate(over="ignore"):
+        for got, x in zip(g.kv_read(1, 70), (k, v)):
+            np.testing.assert_array_equal(got, kvq_plain.values(x).astype(np.float32))
+    assert all(x.shape == (0, 2, 64) for x in g.kv_read(1, 0))
+    with pytest.raises(ad.AdError) as e:
+        g.kv_fill(1, *rows(np.random.default_rng(3), 71, 2, 64))
+    assert e.value.status == ad.AD_ERANGE and g.kv_len(1) == 70
+    g.close()
+
+
 def test_rows_further_apart(ad):
     """ld beyond the rows' own width: what lies between is neither read nor written."""
     import torch
