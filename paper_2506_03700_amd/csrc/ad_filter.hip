@@ -19,7 +19,7 @@
 // What bounds them is not the rows (0.5 MB) but the chain of dependent loads, barriers and kernel boundaries: of a draw from 128256 logits with all three steps on,
 // 24 us in three kernels (2.9, 9.7, 12.0), the last takes 1.0 for its first loads, 1.0 to 1.3 for the classes, 1.2 to publish, 1.5 for the list, 3.3 for the two
 // boundaries, 0.6 to add up, 3.0 to draw.  With every entry of a boundary ranked against all others, and boundaries found through memory, it was 32; ten workgroup-wide steps per boundary in
-// place of two barriers cost 2 more.  A small top-k in one kernel: 12.7 (largest 50).  A row of one segment in
+// place of two barriers cost 2 more.  A small top-k in one kernel: 12.6 (largest 50).  A row of one segment in
 // one kernel: 11.3 us for 2048 logits, 29 in four.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -842,6 +842,19 @@ __global__ void __launch_bounds__(NT) k_filter_row(FilterArgs a) {
     else (void)outcome(a, r, top, kept.least, w, L);
 }
 
+// the distribution of a row of one segment
+__device__ __forceinline__ void write_probs(const FilterArgs &a, int r, const SegLogits &z, const Kept &kept, uint64_t total, float *probs) {
+    const double inv = 1.0 / ldexp((double)total, -a.weight_bits);
+    z.each([&](float x, int j) {
+        if (j < a.V) probs[(size_t)r * a.V + j] = (float)(kept(x, j) * inv);
+    });
+}
+__device__ __forceinline__ void write_no_probs(const FilterArgs &a, int r, const SegLogits &z, float *probs) {
+    z.each([&](float, int j) {
+        if (j < a.V) probs[(size_t)r * a.V + j] = __uint_as_float(0x7fc00000u);
+    });
+}
+
 // A row of one segment: everything, with what the kernels above leave one another in LDS.  It writes the distribution if that is asked for.
 __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
     __shared__ BlockLds L;
@@ -856,9 +869,7 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
     const float top = z.top(L);
     if (!(fabsf(top) < INFINITY)) {
         no_distribution(a, r, top);
-        if (probs) z.each([&](float, int j) {
-            if (j < a.V) probs[(size_t)r * a.V + j] = __uint_as_float(0x7fc00000u);
-        });
+        if (probs) write_no_probs(a, r, z, probs);
         return;
     }
     Kept kept{least_by_weight(a, top), top, a.inv_t};
@@ -909,12 +920,7 @@ __global__ void __launch_bounds__(NT) k_filter_one(FilterArgs a, float *probs) {
         return;
     }
     const uint64_t total = outcome(a, r, top, kept.least, tid == 0 ? mine : 0, L);
-    if (probs) {
-        const double inv = 1.0 / ldexp((double)total, -a.weight_bits);
-        z.each([&](float x, int j) {
-            if (j < a.V) probs[(size_t)r * a.V + j] = (float)(kept(x, j) * inv);
-        });
-    }
+    if (probs) write_probs(a, r, z, kept, total, probs);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -1001,10 +1007,10 @@ __device__ __forceinline__ uint64_t first_k(const FilterArgs &a, Each each, floa
     return lane_u64(mine, __ffsll(__ballot(lane < (int)n && rank == left - 1)) - 1);
 }
 
-// Every workgroup lists its segment's first top_k; the row's last one finds the row's among those and takes the other steps and the draw on what is left, an id a thread.
-// PER: of the list's places, to a thread.
+// Every workgroup lists its segment's first top_k; the row's last one finds the row's among those and takes the other steps and the draw on what is left.
+// PER: of the list's places, to a thread; 0: a row of one segment, which is all there (its distribution too, if that is asked for).
 template <int PER>
-__global__ void __launch_bounds__(NT) k_filter_few(FilterArgs a) {
+__global__ void __launch_bounds__(NT) k_filter_few(FilterArgs a, float *probs) {
     __shared__ BlockLds L;
     __shared__ SelectLds SL;
     __shared__ uint32_t count[kFilterBuckets];
@@ -1024,67 +1030,87 @@ __global__ void __launch_bounds__(NT) k_filter_few(FilterArgs a) {
         });
     }
     __syncthreads();
-    if (tid < a.places) leave(&S.list[r][blockIdx.x * a.places + tid], tid < n_listed ? T[tid] : kUnused);
-    if (tid == 0) leave(&S.seg_top[r][blockIdx.x], seg_top);
-    if (!last_of(S.arrivals[r], a.n_seg, L)) return;
+    float top = seg_top;
+    if constexpr (PER == 0) {
+        if (!(fabsf(top) < INFINITY)) {
+            no_distribution(a, r, top);
+            if (probs) write_no_probs(a, r, z, probs);
+            return;
+        }
+        if (tid < n_listed) key[tid] = key_of(__uint_as_float((uint32_t)(T[tid] >> 32)), (int)(uint32_t)T[tid]);
+    } else {
+        if (tid < a.places) leave(&S.list[r][blockIdx.x * a.places + tid], tid < n_listed ? T[tid] : kUnused);
+        if (tid == 0) leave(&S.seg_top[r][blockIdx.x], seg_top);
+        if (!last_of(S.arrivals[r], a.n_seg, L)) return;
 
-    // (every place of the list is on its way before the first is looked at)
-    uint64_t e[PER];
+        // (every place of the list is on its way before the first is looked at)
+        uint64_t e[PER > 0 ? PER : 1];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) e[i] = tid + i * NT < a.n_seg * a.places ? seen(&S.list[r][tid + i * NT]) : kUnused;
-    bool bad;
-    const float top = row_top<true>(a, r, &bad);
-    if (bad) {
-        no_distribution(a, r, top);
-        return;
+        for (int i = 0; i < PER; ++i) e[i] = tid + i * NT < a.n_seg * a.places ? seen(&S.list[r][tid + i * NT]) : kUnused;
+        bool bad;
+        top = row_top<true>(a, r, &bad);
+        if (bad) {
+            no_distribution(a, r, top);
+            return;
+        }
+        auto listed = [&](auto f) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (e[i] != kUnused) f(__uint_as_float((uint32_t)(e[i] >> 32)), (int)(uint32_t)e[i]);
+        };
+        const uint64_t least_k = first_k(a, listed, top, (uint32_t)a.top_k, count, SL, L);
+        if (tid == 0) n_listed = 0;
+        __syncthreads();
+        listed([&](float x, int id) {
+            const uint64_t k = key_of(x, id);
+            if (k >= least_k) key[atomicAdd(&n_listed, 1)] = k;
+        });
     }
-    auto listed = [&](auto f) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (e[i] != kUnused) f(__uint_as_float((uint32_t)(e[i] >> 32)), (int)(uint32_t)e[i]);
-    };
-    const uint64_t least_k = first_k(a, listed, top, (uint32_t)a.top_k, count, SL, L);
-    if (tid == 0) n_listed = 0;
     __syncthreads();
-    listed([&](float x, int id) {
-        const uint64_t k = key_of(x, id);
-        if (k >= least_k) key[atomicAdd(&n_listed, 1)] = k;
-    });
-    __syncthreads();
-    const int n = n_listed;                                  // top_k, or fewer
-    const uint64_t mine = tid < n ? key[tid] : 0;
-    const double w = tid < n ? weight_of(logit_of(mine), top, a.inv_t) : 0.0;
-    if (tid < n) weight[tid] = whole(w, a.weight_bits);
+    // four threads to an id, each with every fourth of the others (a thread to an id: 128 ids take 1 us more)
+    static_assert(4 * kFilterFew <= NT, "a thread for each quarter");
+    const int n = n_listed, id = tid >> 2, quarter = tid & 3;                    // n: top_k, or fewer
+    const uint64_t mine = id < n ? key[id] : 0;
+    const double w = id < n ? weight_of(logit_of(mine), top, a.inv_t) : 0.0;
+    if (id < n && quarter == 0) weight[id] = whole(w, a.weight_bits);
     T[tid] = 0;
     __syncthreads();
+    auto of_four = [](uint64_t v) {
+        v += dpp_u64<0xB1>(v);
+        return v + dpp_u64<0x4E>(v);
+    };
     // kept: less than top_p of the weight of all before it, and at least min_p of the largest
-    bool keep = tid < n && w >= a.min_p;
-    if (a.top_p < 1.0 && tid < n) {
+    bool keep = id < n && w >= a.min_p;
+    if (a.top_p < 1.0) {
         uint64_t before = 0, all = 0;
-        for (int i = 0; i < n; ++i) {
+        for (int i = quarter; i < n; i += 4) {
             before += key[i] > mine ? weight[i] : 0;
             all += weight[i];
         }
+        before = of_four(before);
+        all = of_four(all);
         keep = keep && before < (uint64_t)ceil(a.top_p * (double)all);
     }
     __syncthreads();
-    if (tid < n && !keep) weight[tid] = 0;
+    if (id < n && !keep && quarter == 0) weight[id] = 0;
     if (!a.tok_out) {
-        if (keep) atomicAdd((unsigned long long *)&T[id_of(mine) / a.seg_ids], (unsigned long long)weight[tid]);
+        if (keep && quarter == 0) atomicAdd((unsigned long long *)&T[id_of(mine) / a.seg_ids], (unsigned long long)weight[id]);
         const uint64_t least = block_extreme<false>(keep ? mine : ~0ull, L);     // (its barriers: the segments' weights are complete)
-        (void)outcome(a, r, top, least, T[tid], L);
+        const uint64_t total = outcome(a, r, top, least, T[tid], L);
+        if (PER == 0 && probs) write_probs(a, r, z, Kept{least, top, a.inv_t}, total, probs);
         return;
     }
     __syncthreads();
-    if (tid >= n) return;
     uint64_t total = 0, ahead = 0;
-    for (int i = 0; i < n; ++i) {
+    for (int i = quarter; i < n; i += 4) {
         total += weight[i];
         ahead += id_of(key[i]) < id_of(mine) ? weight[i] : 0;
     }
+    total = of_four(total);
+    ahead = of_four(ahead);
     uint64_t target = (uint64_t)((double)a.u * (double)total);
     target = target < total ? target : total - 1;
-    if (ahead <= target && target < ahead + weight[tid]) report_draw(a, id_of(mine), (float)(w / ldexp((double)total, -a.weight_bits)));
+    if (id < n && quarter == 0 && ahead <= target && target < ahead + weight[id]) report_draw(a, id_of(mine), (float)(w / ldexp((double)total, -a.weight_bits)));
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -1278,15 +1304,17 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
 int launch_rows(const FilterArgs &a, const LaunchCtx &c, float *probs = nullptr) {
     if (a.V < 1 || a.rows < 1 || a.rows > kFilterRows || a.n_seg > kFilterMaxSegs || !(a.inv_t > 0.0)) return (int)hipErrorInvalidValue;
     const dim3 grid(a.n_seg, a.rows), wg(NT);
+    // (the distribution of 2048 logits by the largest 50 and top-p: 7.7 us, in k_filter_one 11.3)
+    if (a.n_seg == 1 && a.top_k && a.top_k <= kFilterFew) return launch<k_filter_few<0>>(c, grid, wg, 0, a, probs);
     if (a.n_seg == 1) return launch<k_filter_one>(c, dim3(a.rows), wg, 0, a, probs);
-    // A small top-k takes one kernel and not three: a draw from 32016 logits by the largest 128 of them takes 14.4 us where one by the largest 129 takes 22.7,
-    // 8 rows' distributions of 128256 by the largest 50 take 17.9 and by 129 31.0.  The list of fewer places has a shorter program (top-k 50 of
+    // A small top-k takes one kernel and not three: a draw from 32016 logits by the largest 128 of them takes 13.6 us where one by the largest 129 takes 22.7,
+    // 8 rows' distributions of 128256 by the largest 50 take 17.6 and by 129 31.5.  The list of fewer places has a shorter program (top-k 50 of
     // 128256: 12.7 us, and 14.1 with 16 places to a thread); kept in LDS, it leaves a compute unit room for one workgroup (8 rows 27.6).
     if (a.top_k && a.top_k <= kFilterFew && a.top_k * a.n_seg <= kFilterFewList) {
         FilterArgs few = a;
         few.places = a.top_k;
         constexpr int PER = kFilterFewList / NT;
-        return a.top_k * a.n_seg <= kFilterFewList / 2 ? launch<k_filter_few<PER / 2>>(c, grid, wg, 0, few) : launch<k_filter_few<PER>>(c, grid, wg, 0, few);
+        return a.top_k * a.n_seg <= kFilterFewList / 2 ? launch<k_filter_few<PER / 2>>(c, grid, wg, 0, few, (float *)nullptr) : launch<k_filter_few<PER>>(c, grid, wg, 0, few, (float *)nullptr);
     }
     int rc = launch<k_filter_top>(c, grid, wg, 0, a);
     if (rc) return rc;
