@@ -327,7 +327,7 @@ ad_status ad_generate(const ad_model *, ad_kv *, const int32_t *prompt, int32_t 
 
 /* ad_generate in sampled decoding with a filter on every draw and on both sides of every verification; the probability compared with gamma is the
  * filtered distribution's.  The filter's temperature stands in for that of the parameters, whose uniforms are needed.  A filter whose steps are
- * all off is ad_generate at that temperature. */
+ * all off is ad_generate at that temperature.  A final row that has no distribution ends the run with AD_ERANGE. */
 ad_status ad_generate_filtered(const ad_model *, ad_kv *, const int32_t *prompt, int32_t n_prompt, const ad_gen_params *, const ad_filter *,
                                int32_t *out_tokens, int32_t *n_out, ad_stats *stats, ad_event *events, int64_t max_events,
                                int64_t *n_events, void *stream);

@@ -1362,6 +1362,7 @@ struct GpuBackend : Backend {
         filter.temperature = temperature;
         return filter.top_k || (filter.top_p > 0.f && filter.top_p < 1.f) || filter.min_p > 0.f ? &filter : nullptr;
     }
+    static int no_distribution() { return fail(AD_ERANGE, "ad_generate_filtered: a row of logits has no distribution"); }
     // Eq. 1 with a sampled token: the head's logits stay in the draft slot of this row until the verification
     int sample_head(int32_t layer, int32_t r, int32_t, float temperature, float u, int32_t *token, float *prob) override {
         float *z = m->draft_logits + (size_t)r * m->cfg.vocab;
@@ -1370,6 +1371,8 @@ struct GpuBackend : Backend {
         const ad_filter *f = filter_at(temperature);
         if (rc == AD_OK) rc = f ? ad_sample_filtered_wait(m, z, f, u, token, prob, stream) : ad_sample_logits_wait(m, z, temperature, u, token, prob, stream);
         if (rc != AD_OK) return rc;
+        // (an exit head's row without one has a probability that is above no threshold)
+        if (f && *token < 0 && layer == m->cfg.n_layers) return no_distribution();
         if ((rc = fused_health(m, stream))) return rc;
         const int64_t s = m->cfg.dtype == AD_F32 ? 4 : 2;
         bytes += (int64_t)m->cfg.vocab * m->cfg.d_model * s;
@@ -1385,6 +1388,7 @@ struct GpuBackend : Backend {
                    : ad_verify_sampled_wait(m, m->final_logits, m->draft_logits, draft, n, temperature, u_accept, u_resample, u_final, n_accept, next,
                                             ratio, stream);
         if (rc != AD_OK) return rc;
+        if (f && *next < 0) return no_distribution();
         if ((rc = fused_health(m, stream))) return rc;
         const int64_t s = m->cfg.dtype == AD_F32 ? 4 : 2;
         bytes += (int64_t)m->cfg.vocab * m->cfg.d_model * s;

@@ -478,3 +478,17 @@ def test_generation_with_longer_rows(ad, f):
     # logits are off by some 2^-9, weights by 2^-9 / T = 0.04 of themselves: so is a sum of weights, and about as many draws
     assert exact >= 0.85 * n and n == n_new
     g.close()
+
+
+@pytest.mark.parametrize("no_verify", [False, True])
+def test_generation_without_a_distribution(ad, no_verify):
+    """Final logits that are no numbers end a filtered run with an error, not with a token."""
+    s = UNTIED.with_(dtype=synth.F32)
+    w = synth.make_weights(s, seed=0, with_T=True, T_std=0.03)
+    w["final_norm"] = np.full_like(w["final_norm"], np.nan)
+    g = ad.Model(s, w, 64)
+    for gamma, cap in ((2.0, 0), (0.0, 4)):
+        with pytest.raises(ad.AdError) as e:
+            g.ad_generate(synth.make_prompt(s, 0, 20), 8, gamma, cap, temperature=0.5, uniforms=synth.make_uniforms(s, 3, 64), top_k=12, no_verify=no_verify)
+        assert e.value.status == ad.AD_ERANGE and "no distribution" in str(e.value)
+    g.close()
