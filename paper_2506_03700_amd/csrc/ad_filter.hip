@@ -1155,7 +1155,7 @@ struct Residual {
     }
 };
 
-// A segment of the residual per workgroup, the last one draws.  13.1 us for 6 rows of 128256 logits if a draft is rejected, 6 if none is.  The residual takes two
+// A segment of the residual per workgroup, the last one draws.  12.7 us for 6 rows of 128256 logits if a draft is rejected, 6 if none is.  The residual takes two
 // exponentials and a logarithm in 64 bits an id: only the ids that p keeps, gathered first, come that far (all of a wavefront's turns waited for one such id before: 15.2).
 __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
     __shared__ BlockLds L;
@@ -1200,11 +1200,16 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
         };
         // the ids that p keeps, one after the other: few, and the arithmetic behind them is long (segments beyond the usual length: as they come)
         const bool usual = a.seg_ids <= kFilterSegIds;
+        float z[kKeep];
+        if (usual)
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i) z[i] = j0 + tid + i * NT < j1 ? zp[j0 + tid + i * NT] : -INFINITY;
         if (tid == 0) n_kept = 0;
         __syncthreads();
         if (usual)
-            for (int j = j0 + tid; j < j1; j += NT)
-                if (p.kept.holds(zp[j], j)) ids[atomicAdd(&n_kept, 1)] = j;
+#pragma unroll
+            for (int i = 0; i < kKeep; ++i)
+                if (p.kept.holds(z[i], j0 + tid + i * NT)) ids[atomicAdd(&n_kept, 1)] = j0 + tid + i * NT;
         __syncthreads();
         const double first = usual && tid < n_kept ? res(ids[tid]) : -INFINITY;
         double c = first;
@@ -1249,8 +1254,12 @@ __global__ void __launch_bounds__(NT) k_filter_verify(FilterVerifyArgs v) {
             const int i0 = min(s1, s0 + tid * per), i1 = min(s1, i0 + per);
             int e0 = i0, e1 = i1;
             if (usual) {
+                // (per <= kKeep: their logits all on their way at once)
                 unsigned held = 0;
-                for (int j = i0; j < i1; ++j) held |= p.kept.holds(zp[j], j) ? 1u << (j - i0) : 0;
+#pragma unroll
+                for (int i = 0; i < kKeep; ++i) z[i] = i0 + i < i1 ? zp[i0 + i] : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < kKeep; ++i) held |= p.kept.holds(z[i], i0 + i) ? 1u << i : 0;
                 uint64_t all_held;
                 int at = (int)block_scan(__popc(held), L, &all_held);
                 for (int i = 0; i < i1 - i0; ++i)
